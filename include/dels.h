@@ -375,6 +375,80 @@ dls_status dls_unigram_log_prior(const int32_t *tokens, int64_t n, int32_t V, fl
                                  uint64_t *out_counts, float *out_log_prior, void *stream);
 
 /* ---------------------------------------------------------------------------------
+ * Log probabilities of given tokens, with the entropy and the most likely alternatives, of
+ * rows of logits s at temperature T: what a server returns beside the tokens that it
+ * verified, and where a teacher's entries for distillation come from.  With x = s / T,
+ *   lse = log sum_v exp x_v,  logprob_t = x_t - lse,  H = -sum_v p_v log p_v (nats).
+ *   logits           [rows, V] of `dtype`, row_stride >= V elements apart, the entries of a row
+ *                    contiguous; any alignment of the element type
+ *   tokens           [rows] int32, the given token of each row, or NULL (no logprob wanted)
+ *   temperature      finite, > 0
+ *   top_k            number of alternatives, 0 to 256
+ *   out_stats        [rows] dls_token_stats
+ *   out_top_ids      [rows, top_k] int32, by falling logit, equal ones by rising id
+ *   out_top_logprobs [rows, top_k] float32, their log probabilities (both NULL when top_k is 0)
+ *   workspace        at least dls_token_logprobs_workspace_size bytes, 16-byte aligned (may be NULL
+ *                    when that is 0); its content does not matter
+ * -inf marks a masked entry: its probability is 0 and it is no alternative.  A row with fewer than
+ * top_k other entries fills up with id -1 and log probability -inf; a row without any has lse = -inf
+ * and NaN for logprob and entropy.  A token outside [0, V) has logprob NaN, a masked one -inf.
+ * NaN entries are not alternatives.  Finite logits beyond 1e38 T / log2(e) in magnitude count as that
+ * value where the row has no smaller ones.  Limits: 0 <= rows <= 2^20, 1 <= V <= 2^24. */
+typedef struct dls_token_stats {
+  float logprob;
+  float entropy;
+  float lse;
+} dls_token_stats;
+size_t dls_token_logprobs_workspace_size(int64_t rows, int32_t V, int32_t top_k);
+dls_status dls_token_logprobs(const void *logits, dls_dtype dtype, int64_t rows, int32_t V, int64_t row_stride,
+                              const int32_t *tokens, float temperature, int32_t top_k,
+                              dls_token_stats *out_stats, int32_t *out_top_ids, float *out_top_logprobs,
+                              void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------
+ * Distillation of a student from a teacher's top entries.  The teacher gives each row K entries
+ * (id_k, value_k), weights q_k and their mass M = sum_k q_k:
+ *   q = softmax(value / T) over the row's entries (M = 1), or with DLS_TEACHER_LOGPROBS
+ *   q_k = exp(value_k): log probabilities, taken as they are (M <= 1; T is the student's alone)
+ * With student logits s and p = softmax(s / T), the loss of a row and its gradient, for the row's
+ * weight g in the total, are
+ *   loss = sum_k q_k (log q_k - log p[id_k])
+ *   d s_v = g / T (M p_v - sum_{k: id_k = v} q_k)
+ * An entry is absent when its id lies outside [0, V) or its value is -inf; a row without entries has
+ * loss 0 and gradient 0 (a position left out).  Entries of a row may repeat an id.  A masked student
+ * entry (-inf) has p = 0; a teacher entry of positive weight there makes the loss +inf. */
+#define DLS_TEACHER_LOGPROBS 0x1u
+typedef struct dls_teacher {
+  const int32_t *ids;    /* [rows, k] device */
+  const float *values;   /* [rows, k] device, finite or -inf */
+  int32_t k;             /* 1 to 256 */
+  uint32_t flags;        /* DLS_TEACHER_LOGPROBS or 0 */
+  float temperature;     /* T, finite, > 0 */
+  uint32_t reserved;     /* 0 */
+} dls_teacher;
+
+/* Loss, or loss and gradient in one call, of stored logits.
+ *   logits       [rows, V] of `dtype`, row_stride >= V elements apart (any element alignment)
+ *   grad_loss    [rows] float32, g of each row, or NULL (1); read only where out_grad is given
+ *   out_loss     [rows] float32, or NULL
+ *   out_lse      [rows] float32 log-sum-exp of s / T (-inf for a row without entries above
+ *                -inf), or NULL
+ *   out_grad     [rows, V] of `dtype`, grad_stride >= V elements apart, or NULL.  It may be the
+ *                logits themselves (the same pointer and stride): the gradient replaces them.
+ *   workspace    at least dls_distill_workspace_size bytes, 16-byte aligned; its content does not
+ *                matter
+ * dls_distill_grad computes the gradient alone from the log-sum-exps of a loss call (float32
+ * numbers: a probability is then good to the precision of x - lse in float32).
+ * Limits: 0 <= rows <= 2^20, 1 <= V <= 2^24. */
+size_t dls_distill_workspace_size(int64_t rows, int32_t V);
+dls_status dls_distill_loss(const void *logits, dls_dtype dtype, int64_t rows, int32_t V, int64_t row_stride,
+                            dls_teacher teacher, const float *grad_loss, float *out_loss, float *out_lse,
+                            void *out_grad, int64_t grad_stride, void *workspace, size_t ws_bytes, void *stream);
+dls_status dls_distill_grad(const void *logits, dls_dtype dtype, int64_t rows, int32_t V, int64_t row_stride,
+                            const float *lse, dls_teacher teacher, const float *grad_loss, void *out_grad,
+                            int64_t grad_stride, void *stream);
+
+/* ---------------------------------------------------------------------------------
  * Measurement helpers.  They compute nothing of the method: they measure the device's
  * attainable peaks, which benchmarks report beside the vendor figures (8 TB/s HBM,
  * 2.5 PFLOP/s dense bf16) that rooflines are quoted against.  Asynchronous on `stream`;

@@ -476,3 +476,61 @@ def tau_gain_ratio(tau_dels: float, tau_base: float, tau_joint: float) -> float:
 def unigram_log_prior(counts: np.ndarray, smoothing: float = 1.0) -> np.ndarray:
     c = np.asarray(counts, dtype=F64) + F64(smoothing)
     return np.log(c / np.sum(c))
+
+
+# -----------------------------------------------------------------------------------
+# Scoring tokens and teaching a local head, in float64, row by row.
+# -----------------------------------------------------------------------------------
+def _softmax_log(x: np.ndarray):
+    """(log softmax, log-sum-exp) of a row with -inf entries; NaN and -inf where no entry is above -inf."""
+    x = np.asarray(x, np.float64)
+    m = np.max(x)
+    if m == -np.inf:
+        return np.full_like(x, np.nan), -np.inf
+    log_sum = np.log(np.sum(np.exp(x - m)))
+    return x - m - log_sum, m + log_sum   # (m + log_sum would lose the latter where m is the type's lowest value)
+
+
+def token_logprobs_row(logits, token: int, k: int, temperature: float = 1.0):
+    """(logprob, entropy, lse, ids [k], logprobs [k]) of a row: alternatives by falling logit, equal ones by rising
+    index, masked entries never; missing ones are id -1 and -inf."""
+    s = np.asarray(logits, np.float64)
+    logp, lse = _softmax_log(s / temperature)
+    if lse == -np.inf:
+        return np.nan, np.nan, lse, np.full(k, -1, np.int64), np.full(k, -np.inf)
+    p = np.exp(logp)
+    entropy = -float(np.sum(p[p > 0] * logp[p > 0]))
+    order = np.argsort(-s, kind="stable")
+    order = order[s[order] > -np.inf][:k]
+    ids = np.concatenate([order, np.full(k - len(order), -1)])
+    lps = np.concatenate([logp[order], np.full(k - len(order), -np.inf)])
+    return (float(logp[token]) if 0 <= token < len(s) else np.nan), entropy, lse, ids, lps
+
+
+def teacher_weights(ids, values, V: int, temperature: float, renormalise: bool) -> np.ndarray:
+    """q of a row's teacher entries; absent ones (id outside [0, V), value -inf) are 0."""
+    y = np.asarray(values, np.float64)
+    there = (np.asarray(ids) >= 0) & (np.asarray(ids) < V) & (y > -np.inf)
+    q = np.zeros(len(y))
+    if there.any():
+        if renormalise:
+            e = np.exp((y[there] - y[there].max()) / temperature)
+            q[there] = e / e.sum()
+        else:
+            q[there] = np.exp(y[there])
+    return q
+
+
+def distill_row(logits, ids, values, weight: float = 1.0, temperature: float = 1.0, renormalise: bool = True):
+    """(loss, lse, gradient by the logits) of a row; p = 0 at masked entries, in a row without others everywhere."""
+    s = np.asarray(logits, np.float64)
+    ids = np.asarray(ids, np.int64)
+    logp, lse = _softmax_log(s / temperature)
+    if lse == -np.inf:
+        logp = np.full_like(s, -np.inf)
+    q = teacher_weights(ids, values, len(s), temperature, renormalise)
+    on = q > 0
+    loss = float(np.sum(q[on] * (np.log(q[on]) - logp[ids[on]])))
+    grad = q.sum() * np.exp(logp)
+    np.subtract.at(grad, ids[on], q[on])
+    return loss, lse, grad * (weight / temperature)

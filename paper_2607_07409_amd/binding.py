@@ -54,6 +54,15 @@ UNC_ENTROPY, UNC_MAXPROB = 0, 1
 UNC_FIELDS = ("entropy", "max_prob", "u", "gate")
 
 
+TEACHER_LOGPROBS = 0x1
+LOGPROB_FIELDS = ("logprob", "entropy", "lse")
+
+
+class Teacher(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("values", ctypes.c_void_p), ("k", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("temperature", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
 class RowStats(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in STATS_FIELDS]
 
@@ -141,6 +150,17 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     L.dls_draft_block_path.argtypes = [ctypes.POINTER(LocalHeadC), _i32, _i32, ctypes.c_int, ctypes.c_int]
     L.dls_unigram_log_prior.restype = ctypes.c_int
     L.dls_unigram_log_prior.argtypes = [_vp, _i64, _i32, ctypes.c_float, _vp, _vp, _vp]
+    L.dls_token_logprobs_workspace_size.restype = _sz
+    L.dls_token_logprobs_workspace_size.argtypes = [_i64, _i32, _i32]
+    L.dls_token_logprobs.restype = ctypes.c_int
+    L.dls_token_logprobs.argtypes = [_vp, ctypes.c_int, _i64, _i32, _i64, _vp, ctypes.c_float, _i32, _vp, _vp, _vp,
+                                     _vp, _sz, _vp]
+    L.dls_distill_workspace_size.restype = _sz
+    L.dls_distill_workspace_size.argtypes = [_i64, _i32]
+    L.dls_distill_loss.restype = ctypes.c_int
+    L.dls_distill_loss.argtypes = [_vp, ctypes.c_int, _i64, _i32, _i64, Teacher, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]
+    L.dls_distill_grad.restype = ctypes.c_int
+    L.dls_distill_grad.argtypes = [_vp, ctypes.c_int, _i64, _i32, _i64, _vp, Teacher, _vp, _vp, _i64, _vp]
     L.dls_accept_len.restype = ctypes.c_int
     L.dls_accept_len.argtypes = [_vp, _vp, _i32, _i32, _vp, _vp]
     L.dls_measure_read.restype = ctypes.c_int
@@ -454,6 +474,156 @@ def unigram_log_prior(tokens: torch.Tensor, V: int, smoothing: float = 1.0, out=
     _check(L.dls_unigram_log_prior(_ptr(tokens) if n else None, n, V, smoothing, _ptr(counts), _ptr(logp),
                                    _stream(stream)))
     return logp, counts
+
+
+# -----------------------------------------------------------------------------------
+# scoring tokens and teaching a local head
+# -----------------------------------------------------------------------------------
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements between the rows of a [rows, V] tensor whose rows are contiguous (they may be a slice of wider ones)."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [rows, V], got {tuple(t.shape)}")
+    rows, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"the entries of a row of {name} must be contiguous")
+    if rows <= 1:
+        return V
+    if t.stride(0) < V:
+        raise ValueError(f"the rows of {name} overlap (stride {t.stride(0)} < {V})")
+    return t.stride(0)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, shape, dtype, device):
+    """The pointer of a dense tensor of the given shape and type on the given device (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _on(device: torch.device, stream):
+    """Where a call allocates and launches: the tensors' GPU, and the given stream, whose memory the caching
+    allocator then hands out again only in that stream's order."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        return torch.cuda.stream(stream)
+    if device.index != torch.cuda.current_device():
+        return torch.cuda.device(device)
+    return contextlib.nullcontext()
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {device}")
+    return workspace
+
+
+def token_logprobs_workspace_size(rows: int, V: int, top_k: int = 0) -> int:
+    return int(lib().dls_token_logprobs_workspace_size(rows, V, top_k))
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
+                   out=None, workspace=None, stream=None):
+    """Log probability of the given token of each row of logits [rows, V] (bf16 or float32; rows may be slices of
+    wider ones) at a temperature, with the row's entropy and log-sum-exp and its top_k most likely entries.
+    tokens [rows] int32, or None.  Returns (stats [rows, 3] float32 with the fields LOGPROB_FIELDS, ids
+    [rows, top_k] int32, logprobs [rows, top_k] float32); out: these three tensors, to be overwritten."""
+    dev = logits.device
+    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
+    k = max(top_k, 0)
+    with _on(dev, stream):
+        if out is None:
+            out = (torch.empty((rows, 3), dtype=torch.float32, device=dev),
+                   torch.empty((rows, k), dtype=torch.int32, device=dev),
+                   torch.empty((rows, k), dtype=torch.float32, device=dev))
+        st, ids, lp = out
+        ws = _scratch(workspace, token_logprobs_workspace_size(rows, V, top_k), dev)
+        _check(lib().dls_token_logprobs(
+            _ptr(logits), dtype, rows, V, stride, _vector(tokens, "tokens", (rows,), torch.int32, dev), temperature, top_k,
+            _vector(st, "stats", (rows, 3), torch.float32, dev), _vector(ids, "ids", (rows, k), torch.int32, dev),
+            _vector(lp, "logprobs", (rows, k), torch.float32, dev), _ptr(ws), ws.numel() * ws.element_size(),
+            _stream(stream)))
+    return st, ids, lp
+
+
+def _teacher(ids, values, rows, temperature, renormalise, device) -> Teacher:
+    if ids.dim() != 2:
+        raise ValueError(f"teacher ids must be [rows, K], got {tuple(ids.shape)}")
+    K = ids.shape[1]
+    return Teacher(_vector(ids, "teacher ids", (rows, K), torch.int32, device),
+                   _vector(values, "teacher values", (rows, K), torch.float32, device), K,
+                   0 if renormalise else TEACHER_LOGPROBS, temperature, 0)
+
+
+def distill_workspace_size(rows: int, V: int) -> int:
+    return int(lib().dls_distill_workspace_size(rows, V))
+
+
+def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, grad_loss: Optional[torch.Tensor] = None,
+                 temperature: float = 1.0, renormalise: bool = True, want_grad: bool = False, out=None, workspace=None,
+                 stream=None):
+    """Distillation loss of student logits [rows, V] from a teacher's top entries (ids [rows, K] int32, values
+    [rows, K] float32): sum_k q_k (log q_k - log softmax(logits / T)[id_k]) with q = softmax(values / T), or
+    q = exp(values) with renormalise=False (log probabilities, as token_logprobs gives them).  Entries with an id
+    outside [0, V) or the value -inf are absent.  Returns (loss [rows], lse [rows], grad): with want_grad the
+    gradient [rows, V] by the logits, each row weighted by grad_loss [rows] (None: 1), else None.  out: (loss, lse,
+    grad) to be overwritten; grad may be `logits` itself."""
+    dev = logits.device
+    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
+    with _on(dev, stream):
+        if out is None:
+            out = (torch.empty(rows, dtype=torch.float32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev),
+                   torch.empty((rows, V), dtype=logits.dtype, device=dev) if want_grad else None)
+        loss, lse, grad = out
+        ws = _scratch(workspace, distill_workspace_size(rows, V), dev)
+        gptr, gstride = _grad_rows(grad, logits)
+        _check(lib().dls_distill_loss(
+            _ptr(logits), dtype, rows, V, stride, _teacher(ids, values, rows, temperature, renormalise, dev),
+            _vector(grad_loss, "grad_loss", (rows,), torch.float32, dev), _vector(loss, "loss", (rows,), torch.float32, dev),
+            _vector(lse, "lse", (rows,), torch.float32, dev), gptr, gstride, _ptr(ws), ws.numel() * ws.element_size(),
+            _stream(stream)))
+    return loss, lse, grad
+
+
+def _grad_rows(grad: Optional[torch.Tensor], logits: torch.Tensor):
+    if grad is None:
+        return None, 0
+    if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device:
+        raise ValueError("the gradient must have the logits' shape, type and device")
+    return _ptr(grad), _row_stride(grad, "grad")
+
+
+def distill_grad(logits: torch.Tensor, lse: torch.Tensor, ids: torch.Tensor, values: torch.Tensor,
+                 grad_loss: Optional[torch.Tensor] = None, temperature: float = 1.0, renormalise: bool = True, out=None,
+                 stream=None) -> torch.Tensor:
+    """Gradient of distill_loss by the logits, from the log-sum-exps [rows] that it returned, each row weighted by
+    grad_loss [rows] (None: 1).  out: the tensor to be overwritten (may be `logits` itself)."""
+    dev = logits.device
+    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
+        gptr, gstride = _grad_rows(out, logits)
+        _check(lib().dls_distill_grad(
+            _ptr(logits), dtype, rows, V, stride, _vector(lse, "lse", (rows,), torch.float32, dev),
+            _teacher(ids, values, rows, temperature, renormalise, dev),
+            _vector(grad_loss, "grad_loss", (rows,), torch.float32, dev), gptr, gstride, _stream(stream)))
+    return out
 
 
 MEASURE_READ_WORDS = 8192

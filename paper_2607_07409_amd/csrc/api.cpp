@@ -9,18 +9,23 @@
 #include <mutex>
 #include <type_traits>
 
+#include "api_util.hpp"
 #include "dels_internal.hpp"
 #include "peaks.hpp"
 
-namespace {
+using namespace dls::abi;
 
 // Process-lifetime state of the library is trivially destructible (plain arrays and flags):
 // the library registers no destructor that would run at process exit.
+namespace {
 thread_local char g_last_error[512];
+}
+
+namespace dls {
+namespace abi {
 
 void clear_error() { g_last_error[0] = 0; }
 
-dls_status fail(dls_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 dls_status fail(dls_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -29,7 +34,14 @@ dls_status fail(dls_status s, const char* fmt, ...) {
   return s;
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+dls_status hip_fail(hipError_t e, const char* what) {
+  return fail(DLS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+}  // namespace abi
+}  // namespace dls
+
+namespace {
 
 // Device check: a visible gfx950 device must be current.  The result for each device
 // id is computed once; it never changes during the life of the process.
@@ -42,7 +54,9 @@ struct DevInfo {
 static_assert(std::is_trivially_destructible<DevInfo>::value, "no exit-time destructor");
 DevInfo g_dev[64];
 
-dls_status check_device(int* cus = nullptr) {
+}  // namespace
+
+dls_status dls::abi::check_device(int* cus) {
   int n = 0;
   hipError_t e = hipGetDeviceCount(&n);
   if (e != hipSuccess || n <= 0) return fail(DLS_ERR_DEVICE, "no HIP device available (%s)", hipGetErrorString(e));
@@ -72,24 +86,10 @@ dls_status check_device(int* cus = nullptr) {
   return DLS_OK;
 }
 
+namespace {
+
 // number of persistent workgroups for this device (0: no cooperative launch)
 int persist_groups(int cus) { return std::min(cus, dls::kMaxG); }
-
-dls_status hip_fail(hipError_t e, const char* what) {
-  return fail(DLS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-// An enum from a C caller may hold any int; loading an out-of-range value as the C++ enum is
-// undefined, so caller-supplied enums are read through their representation until validated.
-template <typename E>
-int enum_bits(const E& e) {
-  static_assert(sizeof(E) == sizeof(int), "the C enums of the ABI are int-sized");
-  int v;
-  std::memcpy(&v, &e, sizeof v);
-  return v;
-}
-
-bool valid_dtype(int t) { return t == DLS_F32 || t == DLS_BF16; }
 
 dls_status check_fusion(const dls_fusion& f) {
   if (!std::isfinite(f.w_long) || !std::isfinite(f.alpha) || !std::isfinite(f.beta))

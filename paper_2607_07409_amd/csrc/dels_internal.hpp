@@ -73,6 +73,55 @@ int uncertainty_parts(int64_t rows, int32_t V);
 size_t uncertainty_workspace_bytes(int64_t rows, int32_t V);
 hipError_t launch_uncertainty(const UncArgs& a, hipStream_t st);
 
+// log probabilities of given tokens, entropy, alternatives (token_logprobs.hip)
+struct LogprobsArgs {
+  const void* logits;
+  dls_dtype dtype;
+  int64_t rows;
+  int32_t V;
+  int64_t stride;            // elements between rows
+  const int32_t* tokens;     // [rows], or NULL
+  float temperature;
+  int32_t k;
+  dls_token_stats* out;
+  int32_t* top_ids;          // [rows, k]
+  float* top_logprobs;
+  char* ws;                  // logprobs_layout(...).total bytes
+};
+struct LogprobsLayout {
+  size_t off_keys, total;    // sums of the parts first, then their best keys
+};
+LogprobsLayout logprobs_layout(int64_t rows, int32_t V, int elem_bytes, int k);
+hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t st);
+
+// a teacher's top entries of a row, as the distillation kernels take them (teacher.hpp)
+struct TeacherArgs {
+  const int32_t* ids;
+  const float* values;
+  int k;
+  int logprobs;      // values are log probabilities: q = exp(value); otherwise q = softmax(value / T) over the entries
+  float c;           // log2(e) / T
+  float inv_temp;    // 1 / T
+};
+// distillation of stored logits (distill.hip)
+struct DistillArgs {
+  const void* logits;
+  dls_dtype dtype;
+  int64_t rows;
+  int32_t V;
+  int64_t stride;
+  TeacherArgs teacher;
+  const float* weight;       // [rows] or NULL: each row's weight in the total
+  const float* lse;          // the gradient alone: the loss call's log-sum-exps
+  float *out_loss, *out_lse; // [rows] or NULL
+  void* grad;                // [rows, V] of the logits' type, or NULL
+  int64_t grad_stride;
+  char* ws;                  // distill_workspace_bytes (the loss call)
+};
+size_t distill_workspace_bytes(int64_t rows, int32_t V);
+hipError_t launch_distill_loss(const DistillArgs& a, hipStream_t st);
+hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t st);
+
 struct DraftLayout {
   int groups;      // workgroups that share the vocabulary
   size_t off_h0, off_h1, off_rho, off_part, total;

@@ -1,0 +1,209 @@
+// Distillation of rows of student logits s from a teacher's top entries (id_k, q_k), at temperature T:
+//   loss   = sum_k q_k (log q_k - log softmax(s / T)[id_k])
+//   d s_v  = g / T (M softmax(s / T)_v - sum_{k: id_k = v} q_k),   M = sum_k q_k, g the row's weight in the total.
+//
+// The loss needs the row's log-sum-exp, one pass over the logits (row_stream.hpp), and K entries.  The gradient is a
+// second pass that reads an entry and writes one; the teacher's entries of a workgroup's range are written after it,
+// each from its own logit in float32 and rounded once (several entries of one id by the first of them).
+#include "teacher.hpp"
+
+namespace dls {
+
+namespace {
+
+constexpr int kThreads = kRowThreads;
+
+struct LossOut {
+  float *loss, *lse;   // either may be NULL
+  float2* row;         // (R, log2 s) for the gradient pass, or NULL
+};
+
+// the loss of a row from its sums, by the whole workgroup
+template <typename T>
+__device__ __forceinline__ void finish_row(const T* row, int V, int64_t r, const RowSum& a, const TeacherArgs& te,
+                                           TeacherShared& sh, const LossOut& o) {
+  float mass;
+  const TeacherEntry e = teacher_entry(te, r, V, sh, &mass);
+  const float l2 = a.s > 0.f ? fast_log2(a.s) : 0.f;
+  const float x = e.id >= 0 ? to_f32(row[e.id]) : -INFINITY;
+  const float loss = block_sum(teacher_term(e, above_ref(x, te.c, a.R) - l2), sh.red);
+  if (threadIdx.x == 0) {
+    if (o.loss) o.loss[r] = loss;
+    if (o.lse) o.lse[r] = row_lse(a);
+    if (o.row) o.row[r] = make_float2(a.R, l2);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__ L, int V, int64_t stride, TeacherArgs te,
+                                                           float2* __restrict__ part_sums, LossOut o) {
+  constexpr int N = Chunk<T>::N;
+  __shared__ RowShared shr;
+  __shared__ TeacherShared sht;
+  const int part = blockIdx.y, parts = gridDim.y;
+  const int64_t r = blockIdx.x;
+  const T* row = L + (size_t)r * stride;
+  const RowRange g = row_range(row, V, part, parts);
+  RowSum a = row_empty();
+  row_edges(g, V, part, parts, [&](int v) {
+    const float x = to_f32(row[v]);
+    row_fold<1, false>(a, &x, x, te.c);
+  });
+  row_chunks(row, g, [&](int, const float* x, float cm) { row_fold<N, false>(a, x, cm, te.c); }, [](int) {});
+  a = row_block_merge<false>(a, shr);
+  if (parts == 1) finish_row(row, V, r, a, te, sht, o);
+  else if (threadIdx.x == 0) part_sums[(size_t)r * parts + part] = make_float2(a.R, a.s);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_distill_finish(const T* __restrict__ L, int V, int64_t stride,
+                                                             TeacherArgs te, int parts,
+                                                             const float2* __restrict__ part_sums, LossOut o) {
+  __shared__ RowShared shr;
+  __shared__ TeacherShared sht;
+  const int64_t r = blockIdx.x;
+  RowSum a = row_empty();
+  if ((int)threadIdx.x < parts) {   // parts <= 256
+    const float2 p = part_sums[(size_t)r * parts + threadIdx.x];
+    a.R = p.x;
+    a.s = p.y;
+  }
+  a = row_block_merge<false>(a, shr);
+  finish_row(L + (size_t)r * stride, V, r, a, te, sht, o);
+}
+
+// 16-byte stores at any element alignment (the gradient's rows may be aligned otherwise than the logits')
+template <typename T> struct Store;
+template <> struct Store<float> {
+  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+  __device__ __forceinline__ static void chunk(float* p, const float* v) {
+    vec o = {v[0], v[1], v[2], v[3]};
+    __builtin_nontemporal_store(o, reinterpret_cast<vec*>(p));
+  }
+  __device__ __forceinline__ static void one(float* p, float v) { *p = v; }
+};
+template <> struct Store<bf16_t> {
+  typedef __bf16 vec __attribute__((ext_vector_type(8)));
+  typedef float vecf __attribute__((ext_vector_type(8)));
+  typedef unsigned words __attribute__((ext_vector_type(4), aligned(2)));
+  __device__ __forceinline__ static void chunk(bf16_t* p, const float* v) {
+    const vecf f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    __builtin_nontemporal_store(__builtin_bit_cast(words, __builtin_convertvector(f, vec)), reinterpret_cast<words*>(p));
+  }
+  __device__ __forceinline__ static void one(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, int64_t stride, TeacherArgs te,
+                                                           const float* __restrict__ lse,
+                                                           const float2* __restrict__ row_stats,
+                                                           const float* __restrict__ weight, T* G, int64_t gstride) {
+  constexpr int N = Chunk<T>::N;
+  __shared__ TeacherShared sht;
+  __shared__ int ids[kThreads];
+  __shared__ float qs[kThreads];
+  const int part = blockIdx.y, parts = gridDim.y, t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const T* row = L + (size_t)r * stride;
+  T* out = G + (size_t)r * gstride;
+  const RowRange g = row_range(row, V, part, parts);
+  float mass;
+  const TeacherEntry e = teacher_entry(te, r, V, sht, &mass);
+  ids[t] = e.id;
+  qs[t] = e.q;
+  __syncthreads();
+  // softmax(s / T)_v = 2^(y - R) f
+  float R, f;
+  if (row_stats) {
+    const float2 p = row_stats[r];
+    R = p.x;
+    f = R == kNoRef ? 0.f : fast_exp2(-p.y);
+  } else {
+    // lse log2(e) to twice the precision: the part that R cannot hold goes into the factor
+    const float l = lse[r];
+    R = __builtin_amdgcn_fmed3f(l * kLog2e, -kMostY, kMostY);
+    f = l == -INFINITY ? 0.f
+        : fabsf(R) < kPlainRef ? fast_exp2(-(__builtin_fmaf(l, kLog2e, -R) + l * kLog2eLow)) : 1.f;
+  }
+  const float w = (weight ? weight[r] : 1.f) * te.inv_temp;
+  const float a = w * mass * f;
+  // (a clamped R holds no difference of the size of a logarithm: a probability is then at most 1)
+  const float most = fabsf(R) < kPlainRef ? 126.f : 0.f;
+  auto dense = [&](float x) { return a * fast_exp2(fminf(above_ref(x, te.c, R), most)); };
+
+  // my entry, if its id lies in this part's range and no earlier entry has the same id
+  const int lo = part == 0 ? 0 : g.h0 + g.c0 * N, hi = part == parts - 1 ? V : g.h0 + g.c1 * N;
+  bool mine = e.id >= lo && e.id < hi;
+  float entry = 0.f;
+  if (mine) {
+    float q = 0.f;
+    for (int j = 0; j < te.k; ++j) {
+      const bool same = ids[j] == e.id;
+      q += same ? qs[j] : 0.f;
+      mine = mine && !(same && j < t);
+    }
+    entry = dense(to_f32(row[e.id])) - w * q;   // read before anything is written: G may be L
+  }
+  __syncthreads();
+  row_edges(g, V, part, parts, [&](int v) { Store<T>::one(out + v, dense(to_f32(row[v]))); });
+  row_chunks(
+      row, g,
+      [&](int c, const float* x, float) {
+        float d[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] = dense(x[i]);
+        Store<T>::chunk(out + g.h0 + (size_t)c * N, d);
+      },
+      [](int) {});
+  __syncthreads();   // the pass over the range is written before its teacher entries are
+  if (mine) Store<T>::one(out + e.id, entry);
+}
+
+// workgroups per row of the gradient pass: ranges of about 32 KiB, more where rows are few
+int grad_parts(int64_t rows, int32_t V, int elem_bytes) {
+  const int64_t few = row_parts(rows, V, elem_bytes), fit = ((int64_t)V * elem_bytes + 32767) / 32768;
+  return (int)std::max<int64_t>(1, std::max(few, fit));
+}
+
+template <typename T>
+hipError_t launch_grad_t(const DistillArgs& a, const float2* row_stats, hipStream_t st) {
+  const dim3 grid((unsigned)a.rows, (unsigned)grad_parts(a.rows, a.V, (int)sizeof(T)));
+  k_distill_grad<T><<<grid, kThreads, 0, st>>>((const T*)a.logits, a.V, a.stride, a.teacher, a.lse, row_stats, a.weight,
+                                               (T*)a.grad, a.grad_stride);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_loss_t(const DistillArgs& a, hipStream_t st) {
+  const int parts = row_parts(a.rows, a.V, (int)sizeof(T));
+  float2* rows = (float2*)a.ws;
+  float2* sums = rows + a.rows;
+  const LossOut o = {a.out_loss, a.out_lse, a.grad ? rows : nullptr};
+  const T* L = (const T*)a.logits;
+  k_distill_part<T><<<dim3((unsigned)a.rows, (unsigned)parts), kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, sums, o);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (parts > 1) {
+    k_distill_finish<T><<<(unsigned)a.rows, kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, parts, sums, o);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return a.grad ? launch_grad_t<T>(a, rows, st) : hipSuccess;
+}
+
+}  // namespace
+
+size_t distill_workspace_bytes(int64_t rows, int32_t V) {
+  // the larger of the two types' needs: the float32 rows split further
+  const int parts = row_parts(rows, V, 4);
+  return (size_t)rows * sizeof(float2) * (1 + (parts > 1 ? parts : 0));
+}
+
+hipError_t launch_distill_loss(const DistillArgs& a, hipStream_t st) {
+  return a.dtype == DLS_BF16 ? launch_loss_t<bf16_t>(a, st) : launch_loss_t<float>(a, st);
+}
+
+hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t st) {
+  return a.dtype == DLS_BF16 ? launch_grad_t<bf16_t>(a, nullptr, st) : launch_grad_t<float>(a, nullptr, st);
+}
+
+}  // namespace dls

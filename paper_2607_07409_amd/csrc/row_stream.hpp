@@ -1,0 +1,191 @@
+// One pass over rows of logits: what the log-probability and distillation kernels share.
+//
+// A row of V entries is split into `parts` contiguous ranges, one workgroup of 256 threads each.  A thread reads
+// 16-byte chunks (coalesced over the workgroup; the next two are in flight while two are folded) and keeps, for
+// y = x c with c = log2(e) / T,
+//   R   the reference, the largest y so far (rounded as the entries' own products see it),
+//   s   sum 2^(y - R),   and where the entropy is wanted   t = sum 2^(y - R) (y - R),
+// all in float32, so that log-sum-exp = ln2 (R + log2 s), log p = ln2 (y - R - log2 s) and H = ln2 (log2 s - t / s).
+// One fused multiply-add forms y - R with a single rounding, whatever the size of R.
+#pragma once
+#include "dels_internal.hpp"
+#include "stream_load.hpp"
+
+namespace dls {
+
+constexpr int kRowThreads = 256;
+constexpr int kRowUnroll = 2;             // chunks per thread and iteration
+constexpr float kNoRef = -2.0e38f;        // R before the first entry (finite: no inf - inf)
+constexpr float kPlainRef = 0x1p100f;     // |R| below this: y - R is formed by one fma
+constexpr float kMostY = 1.0e38f;         // entries beyond it count as it (only where no entry of the row is plain)
+constexpr float kLog2eLow = 1.92596299e-8f;   // log2(e) - kLog2e
+constexpr float kNoTerm = -1500.f;        // 2^kNoTerm = 0: a lower exponent adds nothing to s or t
+
+struct RowSum {
+  float R, s, t;
+};
+__device__ __forceinline__ RowSum row_empty() { return {kNoRef, 0.f, 0.f}; }
+
+// y - R of one entry; -inf for a masked one.  Rows whose largest entries lie beyond kPlainRef (a row of the
+// type's lowest value, say) take the entries' products clamped, so that nothing overflows.
+__device__ __forceinline__ float above_ref(float x, float c, float R) {
+  if (fabsf(R) < kPlainRef) return __builtin_fmaf(x, c, -R);
+  return x == -INFINITY ? -INFINITY : __builtin_amdgcn_fmed3f(x * c, -kMostY, kMostY) - R;
+}
+
+template <bool ENT>
+__device__ __forceinline__ void row_rescale(RowSum& a, float R) {
+  const float d = fmaxf(a.R - R, kNoTerm), r = fast_exp2(d);
+  if (ENT) a.t = r * __builtin_fmaf(a.s, d, a.t);
+  a.s *= r;
+  a.R = R;
+}
+
+// n entries whose largest is cm
+template <int n, bool ENT>
+__device__ __forceinline__ void row_fold(RowSum& a, const float* x, float cm, float c) {
+  const float R = fmaxf(a.R, cm * c);
+  if (fabsf(R) < kPlainRef) {
+    row_rescale<ENT>(a, R);
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float y = __builtin_fmaf(x[i], c, -R);   // <= 0 up to rounding; -inf for a masked entry
+      const float e = fast_exp2(y);
+      a.s += e;
+      if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
+    }
+  } else if (cm > -INFINITY) {   // nothing plain so far, here neither
+    row_rescale<ENT>(a, fmaxf(a.R, __builtin_amdgcn_fmed3f(cm * c, -kMostY, kMostY)));
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float y = above_ref(x[i], c, a.R), e = fast_exp2(y);
+      a.s += e;
+      if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
+    }
+  }
+}
+
+template <bool ENT>
+__device__ __forceinline__ RowSum row_merge(RowSum a, RowSum b) {
+  const float R = fmaxf(a.R, b.R);
+  row_rescale<ENT>(a, R);
+  row_rescale<ENT>(b, R);
+  return {R, a.s + b.s, ENT ? a.t + b.t : 0.f};
+}
+
+// over the 64 lanes of a wave, the same in every lane: the largest reference first, then one rescale and a sum
+template <bool ENT>
+__device__ __forceinline__ RowSum row_wave_merge(RowSum a) {
+  float R = a.R;
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) R = fmaxf(R, __shfl_xor(R, k));
+  row_rescale<ENT>(a, R);
+  a.s = wave_sum(a.s);
+  if (ENT) a.t = wave_sum(a.t);
+  return a;
+}
+
+// over a workgroup of 256 threads, in a fixed order; every thread gets the total
+struct RowShared {
+  float R[kRowThreads / 64], s[kRowThreads / 64], t[kRowThreads / 64];
+};
+template <bool ENT>
+__device__ __forceinline__ RowSum row_block_merge(RowSum a, RowShared& sh) {
+  a = row_wave_merge<ENT>(a);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    sh.R[wave] = a.R;
+    sh.s[wave] = a.s;
+    if (ENT) sh.t[wave] = a.t;
+  }
+  __syncthreads();
+  RowSum b = {sh.R[0], sh.s[0], ENT ? sh.t[0] : 0.f};
+#pragma unroll
+  for (int w = 1; w < kRowThreads / 64; ++w) b = row_merge<ENT>(b, RowSum{sh.R[w], sh.s[w], ENT ? sh.t[w] : 0.f});
+  return b;
+}
+
+// natural log-sum-exp; -inf for a row without an entry above -inf
+__device__ __forceinline__ float row_lse(const RowSum& a) {
+  return a.s > 0.f ? (a.R + fast_log2(a.s)) * kLn2 : -INFINITY;
+}
+
+// entries before the row's first 16-byte boundary
+template <typename T>
+__device__ __forceinline__ int row_head(const T* p, int V) {
+  const int h = (int)(((16u - ((uint32_t)(uintptr_t)p & 15u)) & 15u) / sizeof(T));
+  return h < V ? h : V;
+}
+
+// the part of a row that a workgroup reads: chunks [c0, c1), entry h0 + c N first in chunk c; the first part has
+// the row's h0 head entries as well, the last one the entries from tail0 on
+struct RowRange {
+  int h0, c0, c1, tail0;
+};
+template <typename T>
+__device__ __forceinline__ RowRange row_range(const T* row, int V, int part, int parts) {
+  constexpr int N = Chunk<T>::N;
+  RowRange r;
+  r.h0 = row_head(row, V);
+  const int nch = (V - r.h0) / N;
+  r.tail0 = r.h0 + nch * N;
+  r.c0 = (int)((int64_t)nch * part / parts);
+  r.c1 = (int)((int64_t)nch * (part + 1) / parts);
+  return r;
+}
+// the head and tail entries of this part: f(index) by the thread that has one
+template <typename F>
+__device__ __forceinline__ void row_edges(const RowRange& r, int V, int part, int parts, F f) {
+  const int t = threadIdx.x;
+  if (part == 0 && t < r.h0) f(t);
+  if (part == parts - 1 && t < V - r.tail0) f(r.tail0 + t);
+}
+
+template <int n>
+__device__ __forceinline__ float max_of(const float* x) {
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < n; ++i) m = fmaxf(m, x[i]);
+  return m;
+}
+
+// Every chunk of the range through `fold(chunk, entries, largest)`, iteration by iteration; `pass(iteration)` after
+// each.  Loads run an iteration ahead (chunks past the range clamped to its last: loaded, never folded).
+template <typename T, typename Fold, typename Pass>
+__device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold fold, Pass pass) {
+  constexpr int N = Chunk<T>::N, NT = kRowThreads;
+  if (r.c1 <= r.c0) return;
+  const int t = threadIdx.x, last = r.c1 - 1;
+  const T* base = row + r.h0;
+  uint4 raw[kRowUnroll];
+#pragma unroll
+  for (int u = 0; u < kRowUnroll; ++u) raw[u] = stream_load16(base + (size_t)min(r.c0 + t + u * NT, last) * N);
+  int it = 0;
+  for (int b = r.c0; b < r.c1; b += NT * kRowUnroll, ++it) {
+    uint4 next[kRowUnroll];
+#pragma unroll
+    for (int u = 0; u < kRowUnroll; ++u)
+      next[u] = stream_load16(base + (size_t)min(b + t + (kRowUnroll + u) * NT, last) * N);
+#pragma unroll
+    for (int u = 0; u < kRowUnroll; ++u) {
+      const int c = b + t + u * NT;
+      if (c < r.c1) {
+        float x[N];
+        Chunk<T>::widen(raw[u], x);
+        fold(c, x, max_of<N>(x));
+      }
+    }
+    pass(it);
+#pragma unroll
+    for (int u = 0; u < kRowUnroll; ++u) raw[u] = next[u];
+  }
+}
+
+// workgroups per row: about four per CU when rows are few, each range at least two chunks a thread
+inline int row_parts(int64_t rows, int32_t V, int elem_bytes) {
+  const int64_t p = (1024 + rows - 1) / std::max<int64_t>(rows, 1);
+  const int64_t cap = V / (kRowThreads * kRowUnroll * (16 / elem_bytes));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(p, cap), 256));
+}
+
+}  // namespace dls

@@ -1,0 +1,319 @@
+// Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits.
+//
+// One pass (row_stream.hpp) gives the log-sum-exp and the entropy.  The alternatives come out of the same pass: the
+// chunks that a thread folds are grouped into blocks, and of each block the pass keeps the largest entry's value and
+// chunk.  Ordered by (value, lower chunk first), the k-th of these block maxima bounds the row's k best entries from
+// below: k blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.
+// Only the k best blocks are read again (from the caches), their entries at or above the bound are collected in LDS,
+// and the k best of those are put in order.  Nothing in the pass depends on the data, so a row of equal entries costs
+// what any other does.
+//
+// Keys: a value's bits as an integer of the same order in the upper half, the complement of the index (or chunk) in
+// the lower, so that the larger key is the better entry, ties going to the lower index, and no two are equal.  0 is
+// no key.  Masked entries (-inf) and NaN have none.
+#include "row_stream.hpp"
+
+namespace dls {
+
+namespace {
+
+constexpr int kThreads = kRowThreads;
+constexpr int kCand = 1024;       // candidates held in LDS; rows with more are selected from by re-reading them
+constexpr int kMostSegs = 4;      // blocks per thread
+
+typedef unsigned long long u64;
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);   // -0 and 0 are one value
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(u64 key) {
+  const uint32_t o = (uint32_t)(key >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ u64 key_of(float x, int index) {
+  return x > -INFINITY ? ((u64)order_of(x) << 32) | (uint32_t)~(uint32_t)index : 0;
+}
+__device__ __forceinline__ int index_of(u64 key) { return (int)~(uint32_t)key; }
+
+struct Select {
+  uint32_t hist[256], wsum[kThreads / 64];
+  uint32_t digit, need, whole;
+  int count;
+};
+
+// The k-th largest of the workgroup's keys (a bound that exactly k keys reach), or 1 where there are fewer than k;
+// `each(f)` calls f with every key of this thread.  Digit by digit from the top, until a digit's keys are all wanted.
+template <typename Each>
+__device__ u64 kth_key(Each each, int k, Select& sh) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  u64 prefix = 0;
+  uint32_t need = (uint32_t)k;
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    sh.hist[t] = 0;
+    __syncthreads();
+    each([&](u64 key) {
+      if (key && (shift == 56 || (key >> (shift + 8)) == prefix)) atomicAdd(&sh.hist[(key >> shift) & 255], 1u);
+    });
+    __syncthreads();
+    const uint32_t h = sh.hist[t];   // thread t owns digit t
+    uint32_t from = h;               // keys with a digit of at least t
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_down(from, d);
+      if (lane + d < 64) from += o;
+    }
+    if (lane == 0) sh.wsum[wave] = from;
+    __syncthreads();
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w)
+      if (w > wave) from += sh.wsum[w];
+    if (from >= need && from - h < need) {
+      sh.digit = (uint32_t)t;
+      sh.need = need - (from - h);
+      sh.whole = h == need - (from - h);
+    }
+    if (t == 0 && from < need) sh.digit = 256;
+    __syncthreads();
+    if (sh.digit == 256) return 1;
+    prefix = (prefix << 8) | sh.digit;
+    need = sh.need;
+    if (sh.whole || shift == 0) return prefix << shift;
+  }
+  return 1;
+}
+
+// The k best of the keys that `each` gives, into out(rank, key), best first; missing ones as key 0.  `list` holds
+// kCand keys; at most k (<= 256) are ordered, each by the number of better ones.
+template <typename Each, typename Out>
+__device__ void best_keys(Each each, int k, u64* list, Select& sh, Out out) {
+  const int t = threadIdx.x;
+  const u64 bound = kth_key(each, k, sh);
+  __syncthreads();
+  if (t == 0) sh.count = 0;
+  __syncthreads();
+  each([&](u64 key) {
+    if (key && key >= bound) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < kCand) list[at] = key;
+    }
+  });
+  __syncthreads();
+  const int n = min(sh.count, k);
+  if (t < n) {
+    const u64 mine = list[t];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > mine;
+    out(rank, mine);
+  } else if (t < k) {
+    out(t, (u64)0);
+  }
+}
+
+struct RowOut {
+  const int32_t* tokens;
+  float c, inv_temp;
+  int k;
+  dls_token_stats* stats;
+  int32_t* ids;
+  float* logprobs;
+};
+
+// log p of an entry: from its distance to the reference, or where that is no float32 number (an entry of the type's
+// lowest value in a row of others) from x / T and the log-sum-exp
+__device__ __forceinline__ float log_p(const RowOut& o, const RowSum& a, float x, float l2) {
+  const float y = above_ref(x, o.c, a.R);
+  return y > -kMostY ? kLn2 * (y - l2) : x * o.inv_temp - kLn2 * (a.R + l2);
+}
+
+// the results of a row
+template <typename T>
+__device__ __forceinline__ void put_stats(const RowOut& o, const T* row, int V, int64_t r, const RowSum& a) {
+  const bool any = a.s > 0.f;
+  const float l2 = fast_log2(a.s), nan = __builtin_nanf("");
+  const int32_t tok = o.tokens ? o.tokens[r] : -1;
+  dls_token_stats st;
+  st.lse = row_lse(a);
+  st.entropy = any ? fmaxf(0.f, kLn2 * (l2 - a.t / a.s)) : nan;
+  st.logprob = any && tok >= 0 && tok < V ? log_p(o, a, to_f32(row[tok]), l2) : nan;
+  o.stats[r] = st;
+}
+__device__ __forceinline__ void put_best(const RowOut& o, int64_t r, const RowSum& a, int rank, u64 key) {
+  const size_t at = (size_t)r * o.k + rank;
+  o.ids[at] = key ? index_of(key) : -1;
+  o.logprobs[at] = key ? log_p(o, a, value_of(key), fast_log2(a.s)) : -INFINITY;
+}
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict__ L, int V, int64_t stride, RowOut o,
+                                                            int segs, float4* __restrict__ part_sums,
+                                                            u64* __restrict__ part_keys) {
+  constexpr int N = Chunk<T>::N, NT = kThreads;
+  __shared__ RowShared shr;
+  __shared__ Select sh;
+  __shared__ u64 blocks[TOP ? kMostSegs * NT : 1];
+  __shared__ u64 list[TOP ? kCand : 1];
+  __shared__ uint16_t chosen[256];
+  const int part = blockIdx.y, parts = gridDim.y, t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const T* row = L + (size_t)r * stride;
+  const RowRange g = row_range(row, V, part, parts);
+  const int iters = (g.c1 - g.c0 + NT * kRowUnroll - 1) / (NT * kRowUnroll);
+  const int per_seg = max(1, (iters + segs - 1) / segs);   // iterations per block
+
+  RowSum a = row_empty();
+  float bm = -INFINITY;   // the block's largest value and its chunk, lowest chunk first
+  int bc = 0;
+  if (TOP)
+    for (int i = t; i < kMostSegs * NT; i += NT) blocks[i] = 0;
+  if (TOP) __syncthreads();
+  row_edges(g, V, part, parts, [&](int v) {
+    const float x = to_f32(row[v]);
+    row_fold<1, true>(a, &x, x, o.c);
+  });
+  row_chunks(
+      row, g,
+      [&](int c, const float* x, float cm) {
+        row_fold<N, true>(a, x, cm, o.c);
+        if (TOP) {
+          bc = cm > bm ? c : bc;
+          bm = fmaxf(bm, cm);
+        }
+      },
+      [&](int it) {
+        if (TOP && (it % per_seg == per_seg - 1 || it == iters - 1)) {
+          blocks[(it / per_seg) * NT + t] = key_of(bm, bc);
+          bm = -INFINITY;
+        }
+      });
+  a = row_block_merge<true>(a, shr);
+  if (t == 0) {
+    if (parts == 1) put_stats(o, row, V, r, a);
+    else part_sums[(size_t)r * parts + part] = make_float4(a.R, a.s, a.t, 0.f);
+  }
+  if (!TOP) return;
+
+  // the k best blocks
+  const u64 bound = kth_key([&](auto f) {
+    for (int i = t; i < segs * NT; i += NT) f(blocks[i]);
+  }, o.k, sh);
+  __syncthreads();
+  if (t == 0) sh.count = 0;
+  __syncthreads();
+  for (int i = t; i < segs * NT; i += NT)
+    if (blocks[i] && blocks[i] >= bound) chosen[atomicAdd(&sh.count, 1)] = (uint16_t)i;   // at most k <= 256
+  __syncthreads();
+  const int nb = sh.count, units = per_seg * kRowUnroll;
+  // their entries, and the row's edge entries, as keys
+  auto entries = [&](auto f) {
+    row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
+    for (int w = t; w < nb * units; w += NT) {
+      const int blk = chosen[w / units], j = w % units;
+      const int c = g.c0 + ((blk / NT) * per_seg * kRowUnroll + j) * NT + blk % NT;
+      if (c >= g.c1) continue;
+      float x[N];
+      Chunk<T>::load(row + g.h0 + (size_t)c * N, x);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (key_of(x[i], c) >= bound) f(key_of(x[i], g.h0 + c * N + i));
+    }
+  };
+  __syncthreads();
+  if (t == 0) sh.count = 0;
+  __syncthreads();
+  entries([&](u64 key) {
+    if (key) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < kCand) list[at] = key;
+    }
+  });
+  __syncthreads();
+  const int n = sh.count;
+  auto put = [&](int rank, u64 key) {
+    if (parts == 1) put_best(o, r, a, rank, key);
+    else part_keys[((size_t)r * parts + part) * o.k + rank] = key;
+  };
+  if (n > kCand) {   // too many at or above the bound (k blocks that hold most of the row's large entries)
+    best_keys(entries, o.k, list, sh, put);
+  } else if (n > o.k) {
+    __shared__ u64 best[256];
+    best_keys([&](auto f) {
+      for (int i = t; i < n; i += NT) f(list[i]);
+    }, o.k, best, sh, put);
+  } else if (t < n) {
+    const u64 mine = list[t];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > mine;
+    put(rank, mine);
+  } else if (t < o.k) {
+    put(t, (u64)0);
+  }
+}
+
+// rows split into parts: one workgroup per row merges the parts' sums and their k best keys
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict__ L, int V, int64_t stride, RowOut o,
+                                                             int parts, const float4* __restrict__ part_sums,
+                                                             const u64* __restrict__ part_keys) {
+  __shared__ RowShared shr;
+  __shared__ Select sh;
+  __shared__ u64 list[TOP ? kCand : 1];
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  RowSum a = row_empty();
+  if (t < parts) {   // parts <= 256
+    const float4 p = part_sums[(size_t)r * parts + t];
+    a = RowSum{p.x, p.y, p.z};
+  }
+  a = row_block_merge<true>(a, shr);
+  if (t == 0) put_stats(o, L + (size_t)r * stride, V, r, a);
+  if (!TOP) return;
+  const u64* keys = part_keys + (size_t)r * parts * o.k;
+  const int n = parts * o.k;
+  best_keys([&](auto f) {
+    for (int i = t; i < n; i += kThreads) f(keys[i]);
+  }, o.k, list, sh, [&](int rank, u64 key) { put_best(o, r, a, rank, key); });
+}
+
+// With alternatives wanted, a merge reads parts x k keys: at most about 2,048 of them
+int logprobs_parts(int64_t rows, int32_t V, int elem_bytes, int k) {
+  const int p = row_parts(rows, V, elem_bytes);
+  return k > 0 ? std::max(1, std::min(p, 2048 / k)) : p;
+}
+
+template <typename T>
+hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
+  const int parts = logprobs_parts(a.rows, a.V, (int)sizeof(T), a.k);
+  const dim3 grid((unsigned)a.rows, (unsigned)parts);
+  const RowOut o = {a.tokens, kLog2e / a.temperature, 1.f / a.temperature, a.k, a.out, a.top_ids, a.top_logprobs};
+  const LogprobsLayout l = logprobs_layout(a.rows, a.V, (int)sizeof(T), a.k);
+  float4* sums = (float4*)a.ws;
+  u64* keys = (u64*)(a.ws + l.off_keys);
+  const int segs = a.k <= 32 ? 1 : kMostSegs;
+  const T* L = (const T*)a.logits;
+  if (a.k > 0) k_logprobs_part<T, true><<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
+  else k_logprobs_part<T, false><<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  if (a.k > 0) k_logprobs_merge<T, true><<<(unsigned)a.rows, kThreads, 0, st>>>(L, a.V, a.stride, o, parts, sums, keys);
+  else k_logprobs_merge<T, false><<<(unsigned)a.rows, kThreads, 0, st>>>(L, a.V, a.stride, o, parts, sums, keys);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+LogprobsLayout logprobs_layout(int64_t rows, int32_t V, int elem_bytes, int k) {
+  const int parts = logprobs_parts(rows, V, elem_bytes, k);
+  LogprobsLayout l = {0, 0};
+  if (parts > 1) {
+    l.off_keys = (size_t)rows * parts * sizeof(float4);
+    l.total = l.off_keys + (size_t)rows * parts * k * sizeof(u64);
+  }
+  return l;
+}
+
+hipError_t launch_logprobs(const LogprobsArgs& a, hipStream_t st) {
+  return a.dtype == DLS_BF16 ? launch_t<bf16_t>(a, st) : launch_t<float>(a, st);
+}
+
+}  // namespace dls

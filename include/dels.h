@@ -449,6 +449,27 @@ dls_status dls_distill_grad(const void *logits, dls_dtype dtype, int64_t rows, i
                             int64_t grad_stride, void *stream);
 
 /* ---------------------------------------------------------------------------------
+ * The same loss through the vocabulary head: s = rho W^T, with rho the head's low-rank states
+ * (SiLU(W_rank h), or E_M's rows) and W its vocabulary matrix.  The logits are recomputed on the
+ * matrix cores where they are needed and never stored.
+ *   rho          [rows, r] bf16, dense, 16-byte aligned
+ *   w_vocab      [V, r] bf16, dense, 16-byte aligned
+ *   grad_loss    [rows] float32, g of each row, or NULL (1); read only with gradients
+ *   out_loss, out_lse  [rows] float32, either may be NULL
+ *   out_d_rho, out_d_w [rows, r] and [V, r] bf16, 16-byte aligned (d_w is 0 without rows): the gradients of
+ *                sum_rows g loss by rho and by W, or both NULL (the loss alone)
+ *   workspace    at least dls_head_distill_workspace_size bytes, 256-byte aligned; its content does
+ *                not matter (with gradients: rows r 4 bytes for each of up to 256 splits of the
+ *                vocabulary, 8 bytes a teacher entry twice, and small)
+ * Products are exact and summed in float32; within the gradients the probabilities are rounded to
+ * bf16, as the results are.  Results do not depend on anything but the arguments (no atomic sums).
+ * Limits: 0 <= rows <= 2^20, 1 <= V <= 2^20, r a multiple of 8 with 8 <= r <= 256; finite rho and W. */
+size_t dls_head_distill_workspace_size(int64_t rows, int32_t V, int32_t r, int32_t k, int with_gradients);
+dls_status dls_head_distill(const void *rho, const void *w_vocab, int64_t rows, int32_t V, int32_t r,
+                            dls_teacher teacher, const float *grad_loss, float *out_loss, float *out_lse,
+                            void *out_d_rho, void *out_d_w, void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------
  * Measurement helpers.  They compute nothing of the method: they measure the device's
  * attainable peaks, which benchmarks report beside the vendor figures (8 TB/s HBM,
  * 2.5 PFLOP/s dense bf16) that rooflines are quoted against.  Asynchronous on `stream`;

@@ -161,6 +161,10 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     L.dls_distill_loss.argtypes = [_vp, ctypes.c_int, _i64, _i32, _i64, Teacher, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]
     L.dls_distill_grad.restype = ctypes.c_int
     L.dls_distill_grad.argtypes = [_vp, ctypes.c_int, _i64, _i32, _i64, _vp, Teacher, _vp, _vp, _i64, _vp]
+    L.dls_head_distill_workspace_size.restype = _sz
+    L.dls_head_distill_workspace_size.argtypes = [_i64, _i32, _i32, _i32, ctypes.c_int]
+    L.dls_head_distill.restype = ctypes.c_int
+    L.dls_head_distill.argtypes = [_vp, _vp, _i64, _i32, _i32, Teacher, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
     L.dls_accept_len.restype = ctypes.c_int
     L.dls_accept_len.argtypes = [_vp, _vp, _i32, _i32, _vp, _vp]
     L.dls_measure_read.restype = ctypes.c_int
@@ -624,6 +628,37 @@ def distill_grad(logits: torch.Tensor, lse: torch.Tensor, ids: torch.Tensor, val
             _teacher(ids, values, rows, temperature, renormalise, dev),
             _vector(grad_loss, "grad_loss", (rows,), torch.float32, dev), gptr, gstride, _stream(stream)))
     return out
+
+
+def head_distill_workspace_size(rows: int, V: int, r: int, K: int, want_grads: bool = True) -> int:
+    return int(lib().dls_head_distill_workspace_size(rows, V, r, K, int(bool(want_grads))))
+
+
+def head_distill(rho: torch.Tensor, w_vocab: torch.Tensor, ids: torch.Tensor, values: torch.Tensor,
+                 grad_loss: Optional[torch.Tensor] = None, temperature: float = 1.0, renormalise: bool = True,
+                 want_grads: bool = False, out=None, workspace=None, stream=None):
+    """distill_loss of the logits rho @ w_vocab.T (bf16 [rows, r] and [V, r]), which are never stored.  Returns
+    (loss [rows], lse [rows], d_rho [rows, r], d_w [V, r]); the gradients, of the rows' losses weighted by grad_loss
+    (None: 1), only with want_grads, else None.  out: these four, to be overwritten."""
+    dev = rho.device
+    if rho.dim() != 2 or w_vocab.dim() != 2:
+        raise ValueError("rho must be [rows, r] and w_vocab [V, r]")
+    (rows, r), V = rho.shape, w_vocab.shape[0]
+    f32, bf16 = torch.float32, torch.bfloat16
+    with _on(dev, stream):
+        if out is None:
+            out = (torch.empty(rows, dtype=f32, device=dev), torch.empty(rows, dtype=f32, device=dev),
+                   torch.empty((rows, r), dtype=bf16, device=dev) if want_grads else None,
+                   torch.empty((V, r), dtype=bf16, device=dev) if want_grads else None)
+        loss, lse, d_rho, d_w = out
+        teacher = _teacher(ids, values, rows, temperature, renormalise, dev)
+        ws = _scratch(workspace, head_distill_workspace_size(rows, V, r, teacher.k, d_rho is not None or d_w is not None), dev)
+        _check(lib().dls_head_distill(
+            _vector(rho, "rho", (rows, r), bf16, dev), _vector(w_vocab, "w_vocab", (V, r), bf16, dev), rows, V, r, teacher,
+            _vector(grad_loss, "grad_loss", (rows,), f32, dev), _vector(loss, "loss", (rows,), f32, dev),
+            _vector(lse, "lse", (rows,), f32, dev), _vector(d_rho, "d_rho", (rows, r), bf16, dev),
+            _vector(d_w, "d_w", (V, r), bf16, dev), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    return loss, lse, d_rho, d_w
 
 
 MEASURE_READ_WORDS = 8192

@@ -48,6 +48,12 @@ dls_status check_teacher_pointers(const dls_teacher& t) {
   return DLS_OK;
 }
 
+dls_status check_head_sizes(int32_t V, int32_t r) {
+  if (V < 1 || V > dls::kHeadMostTiles * dls::kHeadTile) return fail(DLS_ERR_SHAPE, "V=%d outside [1, 2^20]", V);
+  if (r < 8 || r > 256 || r % 8) return fail(DLS_ERR_SHAPE, "r=%d must be a multiple of 8 in [8, 256]", r);
+  return DLS_OK;
+}
+
 dls::TeacherArgs teacher_args(const dls_teacher& t) {
   return {t.ids, t.values, t.k, (t.flags & DLS_TEACHER_LOGPROBS) ? 1 : 0, (float)(1.4426950408889634 / (double)t.temperature),
           1.f / t.temperature};
@@ -179,6 +185,48 @@ dls_status dls_distill_grad(const void* logits, dls_dtype dtype_in, int64_t rows
   a.grad_stride = grad_stride;
   const hipError_t e = dls::launch_distill_grad(a, (hipStream_t)stream);
   return e == hipSuccess ? DLS_OK : hip_fail(e, "distill_grad launch");
+}
+
+size_t dls_head_distill_workspace_size(int64_t rows, int32_t V, int32_t r, int32_t k, int with_gradients) {
+  if (!size_ok(rows, V) || check_head_sizes(V, r) != DLS_OK || k < 1 || k > kMostK) return 0;
+  return dls::head_layout(rows, V, r, k, with_gradients != 0).total;
+}
+
+dls_status dls_head_distill(const void* rho, const void* w_vocab, int64_t rows, int32_t V, int32_t r, dls_teacher teacher,
+                            const float* grad_loss, float* out_loss, float* out_lse, void* out_d_rho, void* out_d_w,
+                            void* workspace, size_t ws_bytes, void* stream) {
+  clear_error();
+  dls_status s;
+  if ((s = check_rows(rows, V)) != DLS_OK || (s = check_head_sizes(V, r)) != DLS_OK || (s = check_teacher(teacher)) != DLS_OK)
+    return s;
+  const bool grads = out_d_rho || out_d_w;
+  if (rows == 0 && !out_d_w) return DLS_OK;   // (without rows d_w is 0, and d_rho may be NULL)
+  if (rows > 0 && grads && !(out_d_rho && out_d_w)) return fail(DLS_ERR_ARG, "out_d_rho and out_d_w are wanted together");
+  if (!w_vocab || (rows > 0 && !rho)) return fail(DLS_ERR_ARG, "required pointer is NULL");
+  if (!out_loss && !out_lse && !grads) return fail(DLS_ERR_ARG, "no output is wanted");
+  if (rows > 0 && (s = check_teacher_pointers(teacher)) != DLS_OK) return s;
+  if (!aligned(rho, 16) || !aligned(w_vocab, 16) || !aligned(out_d_rho, 16) || !aligned(out_d_w, 16) ||
+      !aligned(out_loss, 4) || !aligned(out_lse, 4) || !aligned(grad_loss, 4))
+    return fail(DLS_ERR_ARG, "misaligned pointer");
+  const size_t need = dls_head_distill_workspace_size(rows, V, r, teacher.k, grads);
+  if (ws_bytes < need) return fail(DLS_ERR_WORKSPACE, "workspace %zu bytes < %zu required", ws_bytes, need);
+  if (need && (!workspace || !aligned(workspace, 256))) return fail(DLS_ERR_ARG, "workspace is NULL or not 256-byte aligned");
+  if ((s = check_device()) != DLS_OK) return s;
+  dls::HeadDistillArgs a;
+  a.rho = rho;
+  a.w = w_vocab;
+  a.rows = rows;
+  a.V = V;
+  a.r = r;
+  a.teacher = teacher_args(teacher);
+  a.weight = grad_loss;
+  a.out_loss = out_loss;
+  a.out_lse = out_lse;
+  a.d_rho = out_d_rho;
+  a.d_w = out_d_w;
+  a.ws = (char*)workspace;
+  const hipError_t e = dls::launch_head_distill(a, (hipStream_t)stream);
+  return e == hipSuccess ? DLS_OK : hip_fail(e, "head_distill launch");
 }
 
 }  // extern "C"

@@ -122,6 +122,27 @@ size_t distill_workspace_bytes(int64_t rows, int32_t V);
 hipError_t launch_distill_loss(const DistillArgs& a, hipStream_t st);
 hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t st);
 
+// distillation through the vocabulary head (head_distill.hip)
+constexpr int kHeadTile = 256;         // vocabulary entries of a workgroup of the weight gradient
+constexpr int kHeadMostTiles = 4096;   // V <= 2^20
+struct HeadDistillArgs {
+  const void *rho, *w;       // bf16 [rows, r], [V, r]
+  int64_t rows;
+  int32_t V, r;
+  TeacherArgs teacher;
+  const float* weight;       // [rows] or NULL
+  float *out_loss, *out_lse; // [rows] or NULL
+  void *d_rho, *d_w;         // bf16, both or neither
+  char* ws;                  // head_layout(...).total bytes
+};
+struct HeadLayout {
+  int splits;                // of the vocabulary, where rho is held
+  int tiles, chunk, chunks;  // of the counting sort of the teacher's entries
+  size_t off_o, off_row, off_coef, off_counts, off_totals, off_list, total;
+};
+HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads);
+hipError_t launch_head_distill(const HeadDistillArgs& a, hipStream_t st);
+
 struct DraftLayout {
   int groups;      // workgroups that share the vocabulary
   size_t off_h0, off_h1, off_rho, off_part, total;

@@ -49,7 +49,7 @@ dls_status check_teacher_pointers(const dls_teacher& t) {
 }
 
 dls_status check_head_sizes(int32_t V, int32_t r) {
-  if (V < 1 || V > dls::kHeadMostTiles * dls::kHeadTile) return fail(DLS_ERR_SHAPE, "V=%d outside [1, 2^20]", V);
+  if (V < 1 || V > dls::kHeadMostV) return fail(DLS_ERR_SHAPE, "V=%d outside [1, 2^20]", V);
   if (r < 8 || r > 256 || r % 8) return fail(DLS_ERR_SHAPE, "r=%d must be a multiple of 8 in [8, 256]", r);
   return DLS_OK;
 }

@@ -124,7 +124,9 @@ hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t st);
 
 // distillation through the vocabulary head (head_distill.hip)
 constexpr int kHeadTile = 256;         // vocabulary entries of a workgroup of the weight gradient
-constexpr int kHeadMostTiles = 4096;   // V <= 2^20
+constexpr int kHeadGroup = 64;         // of a wave
+constexpr int kHeadMostV = 1 << 20;
+constexpr int kHeadMostKeys = kHeadMostV / kHeadGroup;
 struct HeadDistillArgs {
   const void *rho, *w;       // bf16 [rows, r], [V, r]
   int64_t rows;
@@ -137,7 +139,8 @@ struct HeadDistillArgs {
 };
 struct HeadLayout {
   int splits;                // of the vocabulary, where rho is held
-  int tiles, chunk, chunks;  // of the counting sort of the teacher's entries
+  int tiles;                 // of the vocabulary, where W is held
+  int keys, chunk, chunks;   // of the counting sort of the teacher's entries
   size_t off_o, off_row, off_coef, off_counts, off_totals, off_list, total;
 };
 HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads);

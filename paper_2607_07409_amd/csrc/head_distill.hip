@@ -44,23 +44,40 @@ struct Tile {
   static constexpr int kLoads = kTile * kPieces / kThreads;          // per thread
   bf16_t y[kTile * D];
 };
+constexpr int kBuffers = 3;   // one tile is multiplied, two are on their way
 
-// A thread's pieces of a tile, from memory to registers (`row_of(v)` gives the row of Y for tile row v, in range;
-// pieces past r are replaced by the row's first: what they meet in X is 0) and from there to LDS.
+// The streams into LDS bypass the registers: 16 (or 4) bytes a lane from its own address to consecutive places from a
+// wave's LDS address (in M0) on.  The compiler does not count them, so the waits are written out.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+__device__ __forceinline__ void stream_to_lds16(const void* from, uint32_t to) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ void stream_to_lds4(const void* from, uint32_t to) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+// all but this wave's last n streams have arrived
+template <int n>
+__device__ __forceinline__ void stream_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+}
+
+// A wave's share of a tile (`row_of(v)` gives the row of Y for tile row v, in range; pieces past r are replaced by
+// the row's first: what they meet in X is 0)
 template <int D, typename RowOf>
-__device__ __forceinline__ void tile_load(uint4* reg, const bf16_t* Y, int r, RowOf row_of) {
+__device__ __forceinline__ void tile_stream(const Tile<D>& to, const bf16_t* Y, int r, RowOf row_of) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
 #pragma unroll
   for (int q = 0; q < Tile<D>::kLoads; ++q) {
-    const int p = q * kThreads + threadIdx.x;
+    const int p0 = (q * kWaves + wave) * 64, p = p0 + lane;
     const int v = p / Tile<D>::kPieces, g = (p % Tile<D>::kPieces) ^ (v & Tile<D>::kSwizzle);
-    reg[q] = *reinterpret_cast<const uint4*>(Y + (size_t)row_of(v) * r + (g * 8 < r ? g * 8 : 0));
+    stream_to_lds16(Y + (size_t)row_of(v) * r + (g * 8 < r ? g * 8 : 0), lds_address(to.y) + p0 * 16);
   }
-}
-template <int D>
-__device__ __forceinline__ void tile_store(const uint4* reg, Tile<D>& t) {
-#pragma unroll
-  for (int q = 0; q < Tile<D>::kLoads; ++q)
-    *reinterpret_cast<uint4*>(t.y + (q * kThreads + threadIdx.x) * 8) = reg[q];
 }
 
 // the held operand: lane n of tile x has row x0 + 32 x + n, 8 of every 16 columns by its half
@@ -128,6 +145,16 @@ __device__ __forceinline__ bf16x8 pack8(const float* v) {
   return __builtin_convertvector(f, bf16x8);
 }
 
+// An accumulator register times f, in place: written out so that the sums stay in the accumulator registers also where
+// they are rescaled (the compiler moves all of them out and back in every tile otherwise).  acc_settle covers the
+// distance that a matrix instruction's result, and its next addend, must keep to these.
+__device__ __forceinline__ float acc_scale(float a, float f) {
+  float v;
+  asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(a), "=&v"(v) : "v"(f));
+  return a;
+}
+__device__ __forceinline__ void acc_settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // ------------------------------------------------------------------------------------------
 // rho held, W streamed
 // ------------------------------------------------------------------------------------------
@@ -137,7 +164,7 @@ template <int D, bool GRAD>
 __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                           int64_t rows, int V, int r, float c, int splits,
                                                           float2* __restrict__ part_sum, float* __restrict__ part_o) {
-  __shared__ Tile<D> tiles[2];
+  __shared__ Tile<D> tiles[kBuffers];
   const int sp = blockIdx.x % splits;
   const int64_t x0 = (int64_t)(blockIdx.x / splits) * kHold + (threadIdx.x >> 6) * 64;
   const int nt = (V + kTile - 1) / kTile;
@@ -149,15 +176,15 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
   hold_load<D>(xf, rho, x0, rows, r);
   f32x16 o[2][GRAD ? D / 32 : 1] = {};
   float ref[2] = {kNoRef, kNoRef}, sum[2] = {0.f, 0.f};
-  uint4 reg[Tile<D>::kLoads];
-  if (t0 < t1) {
-    tile_load<D>(reg, W, r, row_of(t0));
-    tile_store<D>(reg, tiles[0]);
-  }
-  __syncthreads();
+  tile_stream(tiles[0], W, r, row_of(min(t0, nt - 1)));
+  tile_stream(tiles[1], W, r, row_of(min(t0 + 1, nt - 1)));
+  int at = 0;   // t's buffer
   for (int t = t0; t < t1; ++t) {
-    const Tile<D>& cur = tiles[(t - t0) & 1];
-    tile_load<D>(reg, W, r, row_of(min(t + 1, t1 - 1)));
+    stream_wait<Tile<D>::kLoads>();   // t has arrived; t + 1 may be on its way
+    __syncthreads();                  // everybody's share of it, and everybody is done with t - 1
+    const Tile<D>& cur = tiles[at];
+    tile_stream(tiles[at == 0 ? 2 : at - 1], W, r, row_of(min(t + 2, nt - 1)));
+    at = at == 2 ? 0 : at + 1;
     f32x16 s[2];
     product_s<D>(s, cur, xf);
     if (t == nt - 1) {   // rows of the last tile past V
@@ -177,28 +204,31 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
         const float f = fast_exp2(fmaxf(ref[x] - now, kNoTerm));
         ref[x] = now;
         sum[x] *= f;
-        if (GRAD) {
+        if constexpr (GRAD) {
+          acc_settle();
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float fi = __shfl(f, 8 * (i >> 2) + 4 * h + (i & 3));
 #pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) o[x][GRAD ? dt : 0][i] *= fi;
+            for (int dt = 0; dt < D / 32; ++dt) o[x][dt][i] = acc_scale(o[x][dt][i], fi);
           }
+          acc_settle();
         }
       }
-      float e[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        e[i] = fast_exp2(__builtin_fmaf(s[x][i], c, -ref[x]));
-        sum[x] += e[i];
+      for (int j = 0; j < 2; ++j) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -ref[x]));
+          sum[x] += e[i];
+        }
+        if (GRAD) p[x][j] = pack8(e);
       }
-      p[x][0] = pack8(e);
-      p[x][1] = pack8(e + 8);
     }
     if constexpr (GRAD) product_o<D>(o, cur, p);
-    tile_store<D>(reg, tiles[(t - t0 + 1) & 1]);
-    __syncthreads();
   }
+  stream_wait<0>();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const float total = sum[x] + __shfl_xor(sum[x], 32);
@@ -224,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
 struct HeadOut {
   float *loss, *lse;       // either may be NULL
   bf16_t* d_rho;           // with gradients: [rows, r]
-  float2* row;             //   (R + log2 s, g M / T) of each row
+  float2* row;             //   (R + log2 s, g M / T) of each row, to a whole tile of rows
   float* coef;             //   [rows, K]: -g q_k / T of each entry
 };
 
@@ -301,6 +331,8 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
     if (GRAD) o.row[row] = make_float2(a.R + l2, w * mass);
   }
   if (GRAD) {
+    // no row: 2^-kMostY times 0
+    if (row == rows - 1 && t > 0 && t < kTile && (row + t) / kTile == row / kTile) o.row[row + t] = make_float2(kMostY, 0.f);
     if (t < te.k) o.coef[(size_t)row * te.k + t] = -w * e.q;
     if (wave == 0 && on) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -317,107 +349,112 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
 }
 
 // ------------------------------------------------------------------------------------------
-// the teacher's entries in order of the vocabulary tile: a stable counting sort
+// the teacher's entries in order of the group of 64 vocabulary entries that a wave of k_head_w holds: a stable
+// counting sort (keys <= kHeadMostKeys)
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ int entry_tile(const TeacherArgs& te, int64_t e, int64_t n, int V) {
+extern __shared__ uint32_t key_lds[];   // a word per key
+
+__device__ __forceinline__ int entry_key(const TeacherArgs& te, int64_t e, int64_t n, int V) {
   if (e >= n) return -1;
   const int id = te.ids[e];
-  return id >= 0 && id < V && te.values[e] > -INFINITY ? id / kHold : -1;
+  return id >= 0 && id < V && te.values[e] > -INFINITY ? id / kHeadGroup : -1;
 }
 
-// one wave per chunk of the entries: how many of each tile (tiles <= kMostTiles)
-__global__ __launch_bounds__(64) void k_sort_count(TeacherArgs te, int64_t n, int V, int tiles, int chunk,
+// one wave per chunk of the entries: how many of each key
+__global__ __launch_bounds__(64) void k_sort_count(TeacherArgs te, int64_t n, int V, int keys, int chunk,
                                                    uint32_t* __restrict__ counts) {
-  __shared__ uint32_t cnt[kHeadMostTiles];
   const int lane = threadIdx.x;
-  for (int i = lane; i < tiles; i += 64) cnt[i] = 0;
+  for (int i = lane; i < keys; i += 64) key_lds[i] = 0;
   __syncthreads();
   const int64_t e0 = (int64_t)blockIdx.x * chunk;
   for (int i = lane; i < chunk; i += 64) {
-    const int tile = entry_tile(te, e0 + i, n, V);
-    if (tile >= 0) atomicAdd(&cnt[tile], 1u);
+    const int key = entry_key(te, e0 + i, n, V);
+    if (key >= 0) atomicAdd(&key_lds[key], 1u);
   }
   __syncthreads();
-  for (int i = lane; i < tiles; i += 64) counts[(size_t)blockIdx.x * tiles + i] = cnt[i];
+  for (int i = lane; i < keys; i += 64) counts[(size_t)blockIdx.x * keys + i] = key_lds[i];
 }
 
-// one workgroup per tile: the chunks' counts become places within the tile; totals[tile]
-__global__ __launch_bounds__(kThreads) void k_sort_scan(uint32_t* __restrict__ counts, int chunks, int tiles,
+// exclusive sums of v over a workgroup of NT threads; *all: the total
+template <int NT>
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* wsum, uint32_t* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t up = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(up, d);
+    if (lane >= d) up += o;
+  }
+  __syncthreads();
+  if (lane == 63) wsum[wave] = up;
+  __syncthreads();
+  uint32_t add = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) add += wsum[w];
+    total += wsum[w];
+  }
+  *all = total;
+  return add + up - v;
+}
+
+// one workgroup per key: the chunks' counts become places within the key; totals[key]
+__global__ __launch_bounds__(kThreads) void k_sort_scan(uint32_t* __restrict__ counts, int chunks, int keys,
                                                         uint32_t* __restrict__ totals) {
-  __shared__ uint32_t wsum[kWaves];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  uint32_t before = 0;
+  __shared__ uint32_t wsum[kThreads / 64];
+  uint32_t before = 0, all;
   for (int c0 = 0; c0 < chunks; c0 += kThreads) {
-    const int c = c0 + t;
-    const uint32_t v = c < chunks ? counts[(size_t)c * tiles + blockIdx.x] : 0;
-    uint32_t up = v;   // sum of this and the lower lanes
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(up, d);
-      if (lane >= d) up += o;
-    }
-    if (lane == 63) wsum[wave] = up;
-    __syncthreads();
-    uint32_t add = before, all = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) add += wsum[w];
-      all += wsum[w];
-    }
-    if (c < chunks) counts[(size_t)c * tiles + blockIdx.x] = add + up - v;
+    const int c = c0 + (int)threadIdx.x;
+    const uint32_t v = c < chunks ? counts[(size_t)c * keys + blockIdx.x] : 0;
+    const uint32_t at = before + block_before<kThreads>(v, wsum, &all);
+    if (c < chunks) counts[(size_t)c * keys + blockIdx.x] = at;
     before += all;
-    __syncthreads();
   }
-  if (t == 0) totals[blockIdx.x] = before;
+  if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-// one wave per chunk: entry -> its place, in the order of the entries.  list: (row | place in the tile << 24,
-// coefficient).  The first chunk writes where each tile's list begins (begin[tiles] its end).
-__global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, int V, int tiles, int chunk,
-                                                   const uint32_t* __restrict__ counts,
-                                                   const uint32_t* __restrict__ totals, const float* __restrict__ coef,
-                                                   uint32_t* __restrict__ begin, uint2* __restrict__ list) {
-  __shared__ uint32_t at[kHeadMostTiles];
-  const int lane = threadIdx.x;
-  uint32_t before = 0;
-  for (int i0 = 0; i0 < tiles; i0 += 64) {
-    const int i = i0 + lane;
-    const uint32_t v = i < tiles ? totals[i] : 0;
-    uint32_t up = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(up, d);
-      if (lane >= d) up += o;
-    }
-    if (i < tiles) {
-      at[i] = before + up - v + counts[(size_t)blockIdx.x * tiles + i];
-      if (blockIdx.x == 0) begin[i] = before + up - v;
-    }
-    before += __shfl(up, 63);
+// where each key's list begins; begin[keys] ends the last
+__global__ __launch_bounds__(1024) void k_sort_base(const uint32_t* __restrict__ totals, int keys,
+                                                    uint32_t* __restrict__ begin) {
+  __shared__ uint32_t wsum[16];
+  uint32_t before = 0, all;
+  for (int k0 = 0; k0 < keys; k0 += 1024) {
+    const int k = k0 + (int)threadIdx.x;
+    const uint32_t at = before + block_before<1024>(k < keys ? totals[k] : 0, wsum, &all);
+    if (k < keys) begin[k] = at;
+    before += all;
   }
-  if (blockIdx.x == 0 && lane == 0) begin[tiles] = before;
+  if (threadIdx.x == 0) begin[keys] = before;
+}
+
+// one wave per chunk: entry -> its place, in the order of the entries.  list: (row | place in the group << 24,
+// coefficient)
+__global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, int V, int keys, int chunk,
+                                                   const uint32_t* __restrict__ counts,
+                                                   const uint32_t* __restrict__ begin, const float* __restrict__ coef,
+                                                   uint2* __restrict__ list) {
+  const int lane = threadIdx.x;
+  for (int i = lane; i < keys; i += 64) key_lds[i] = begin[i] + counts[(size_t)blockIdx.x * keys + i];
   __syncthreads();
   const int64_t e0 = (int64_t)blockIdx.x * chunk;
   for (int i = 0; i < chunk; i += 64) {
     const int64_t e = e0 + i + lane;
-    const int tile = entry_tile(te, e, n, V);
-    // lanes of the same tile
-    uint64_t same = __builtin_amdgcn_ballot_w64(tile >= 0);
+    const int key = entry_key(te, e, n, V);
+    uint64_t same = __builtin_amdgcn_ballot_w64(key >= 0);   // lanes of the same key
     if (!same) continue;
 #pragma unroll
-    for (int b = 0; (1 << b) < kHeadMostTiles; ++b) {
-      const bool bit = (tile >> b) & 1;
+    for (int b = 0; (1 << b) < kHeadMostKeys; ++b) {
+      const bool bit = (key >> b) & 1;
       const uint64_t set = __builtin_amdgcn_ballot_w64(bit);
       same &= bit ? set : ~set;
     }
-    if (tile >= 0) {
+    if (key >= 0) {
       const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-      const uint32_t place = at[tile] + rank;
-      list[place] = make_uint2((uint32_t)(e / te.k) | (uint32_t)(te.ids[e] % kHold) << 24, __float_as_uint(coef[e]));
-      // (every lane of the tile has read at[tile]: the wave runs in step, and the barrier orders its LDS accesses)
+      list[key_lds[key] + rank] =
+          make_uint2((uint32_t)(e / te.k) | (uint32_t)(te.ids[e] % kHeadGroup) << 24, __float_as_uint(coef[e]));
     }
     __syncthreads();
-    if (tile >= 0 && (same >> lane) == 1) at[tile] += __popcll(same);   // the last lane of the tile
+    if (key >= 0 && (same >> lane) == 1) key_lds[key] += __popcll(same);   // the last lane of the key
     __syncthreads();
   }
 }
@@ -425,102 +462,121 @@ __global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, in
 // ------------------------------------------------------------------------------------------
 // W held, rho streamed
 // ------------------------------------------------------------------------------------------
+// A wave's own tile of Y, by itself
+template <int D, typename RowOf>
+__device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t* Y, int r, RowOf row_of) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int q = 0; q < Tile<D>::kLoads * kWaves; ++q) {
+    const int p = q * 64 + lane;
+    const int v = p / Tile<D>::kPieces, g = (p % Tile<D>::kPieces) ^ (v & Tile<D>::kSwizzle);
+    stream_to_lds16(Y + (size_t)row_of(v) * r + (g * 8 < r ? g * 8 : 0), lds_address(to.y) + q * 1024);
+  }
+}
+// the left operand of a tile of coefficients q[tile row][held row]: their bf16 values, or what those leave
+__device__ __forceinline__ void coefficients(bf16x8 (&p)[2][2], const float* q, bool rest) {
+  const int n = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = q[(16 * j + 8 * (i >> 2) + 4 * h + (i & 3)) * kHeadGroup + 32 * x + n];
+        if (rest) e[i] -= (float)(__bf16)e[i];
+      }
+      p[x][j] = pack8(e);
+    }
+}
+// this wave's LDS accesses are done (its next stream may overwrite what they read)
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                         int64_t rows, int V, int r, float c,
                                                         const float2* __restrict__ row_stats,
                                                         const uint32_t* __restrict__ begin,
                                                         const uint2* __restrict__ list, bf16_t* __restrict__ d_w) {
-  __shared__ Tile<D> tiles[2];
-  __shared__ float rl[2][kTile], ra[2][kTile];   // of a tile's rows: R + log2 s and g M / T; of entries: place, coefficient
+  // the stream's buffers; after it a tile of each wave
+  static_assert(kBuffers < kWaves, "the waves' own tiles cover the stream's");
+  __shared__ Tile<D> tiles[kWaves];
+  __shared__ float2 stats[kBuffers][kWaves][kTile];   // of a tile's rows, a copy for each wave
+  __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients where a group has many entries
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, t = threadIdx.x;
-  const int64_t x0 = (int64_t)blockIdx.x * kHold + (t >> 6) * 64;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int64_t x0 = (int64_t)blockIdx.x * kHold + wave * 64;
   const int nt = (int)((rows + kTile - 1) / kTile);
-  const uint32_t b0 = begin[blockIdx.x], b1 = begin[blockIdx.x + 1];
-  const int ne = (int)((b1 - b0 + kTile - 1) / kTile);
-  auto row_of = [&](int tile) { return [=](int v) { return (int)min((int64_t)tile * kTile + v, rows - 1); }; };
-  auto entry_of = [&](int tile) {   // (a tile of entries has at least one)
-    return [=](int v) { return (int)(list[min(b0 + (uint32_t)tile * kTile + v, b1 - 1)].x & 0xffffffu); };
-  };
-  auto stats_of = [&](int tile) {
-    const int64_t row = (int64_t)tile * kTile + t;
-    return t < kTile && row < rows ? row_stats[row] : make_float2(kMostY, 0.f);   // no row: 2^-kMostY times 0
+  auto stream = [&](int tile, int to) {
+    stream_to_lds4((const float*)(row_stats + (size_t)tile * kTile) + lane, lds_address(stats[to][wave]));
+    tile_stream(tiles[to], rho, r, [=](int v) { return (int)min((int64_t)tile * kTile + v, rows - 1); });
   };
 
   bf16x8 xf[2][D / 16];
   hold_load<D>(xf, W, x0, V, r);
   f32x16 o[2][D / 32] = {};
-  uint4 reg[Tile<D>::kLoads];
-  tile_load<D>(reg, rho, r, row_of(0));
-  tile_store<D>(reg, tiles[0]);
-  if (t < kTile) {
-    const float2 st = stats_of(0);
-    rl[0][t] = st.x;
-    ra[0][t] = st.y;
-  }
-  __syncthreads();
+  stream(0, 0);
+  stream(min(1, nt - 1), 1);
+  int at = 0;
   for (int k = 0; k < nt; ++k) {
-    const Tile<D>& cur = tiles[k & 1];
-    const int next = min(k + 1, nt - 1);
-    tile_load<D>(reg, rho, r, row_of(next));
-    const float2 st = stats_of(next);
+    stream_wait<Tile<D>::kLoads + 1>();
+    __syncthreads();
+    const Tile<D>& cur = tiles[at];
+    const float2* st = stats[at][wave];
+    stream(min(k + 2, nt - 1), at == 0 ? 2 : at - 1);
+    at = at == 2 ? 0 : at + 1;
     f32x16 s[2];
     product_s<D>(s, cur, xf);
     bf16x8 p[2][2];
-    float l[16], a[16];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int j = 0; j < 2; ++j) {
+      float e[2][8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        l[4 * q + i] = rl[k & 1][8 * q + 4 * h + i];
-        a[4 * q + i] = ra[k & 1][8 * q + 4 * h + i];
+      for (int i = 0; i < 8; ++i) {
+        const float2 la = st[16 * j + 8 * (i >> 2) + 4 * h + (i & 3)];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) e[x][i] = la.y * fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -la.x));
       }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float e[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) e[i] = a[i] * fast_exp2(__builtin_fmaf(s[x][i], c, -l[i]));
-      p[x][0] = pack8(e);
-      p[x][1] = pack8(e + 8);
+      p[0][j] = pack8(e[0]);
+      p[1][j] = pack8(e[1]);
     }
     product_o<D>(o, cur, p);
-    tile_store<D>(reg, tiles[(k + 1) & 1]);
-    if (t < kTile) {
-      rl[(k + 1) & 1][t] = st.x;
-      ra[(k + 1) & 1][t] = st.y;
-    }
-    __syncthreads();
   }
-  // the teacher's entries of this tile
-  for (int k = 0; k < ne; ++k) {
-    tile_load<D>(reg, rho, r, entry_of(k));
-    tile_store<D>(reg, tiles[0]);
-    if (t < kTile) {
-      const uint32_t i = b0 + (uint32_t)k * kTile + t;
-      const uint2 en = i < b1 ? list[i] : make_uint2(0u, 0u);
-      rl[0][t] = (float)(en.x >> 24);
-      ra[0][t] = __uint_as_float(en.y);
-    }
-    __syncthreads();
-    bf16x8 hi[2][2], lo[2][2];
+  stream_wait<0>();
+  __syncthreads();
+  // The teacher's entries of this wave's 64 rows of W, in order of the row.  Few of them: 32 entries a tile, each with
+  // its own row of rho and one coefficient.  Many (frequent tokens): by tiles of 32 successive rows, with all of a
+  // tile's coefficients, so that no group takes longer than the rows did.
+  const uint32_t b0 = begin[blockIdx.x * kWaves + wave], b1 = begin[blockIdx.x * kWaves + wave + 1];
+  const Tile<D>& own = tiles[wave];
+  float* q = wide[wave];
+  const bool few = (b1 - b0 + kTile - 1) / kTile <= (uint32_t)nt;
+  for (uint32_t b = b0; b < b1;) {
+    uint2 en = list[min(b + lane, b1 - 1)];
+    const uint32_t tile = __builtin_amdgcn_readfirstlane(en.x & 0xffffffu) / kTile;
+    const int mine = few ? (int)(en.x & 0xffffffu) : (int)min((int64_t)tile * kTile + n, rows - 1);   // lane m: tile row m's
+    lds_done();
+    wave_tile_stream(own, rho, r, [&](int v) { return __shfl(mine, v); });
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float place = (float)((t >> 6) * 64 + 32 * x + n);
-      float e[16], f[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int m = 8 * (i >> 2) + 4 * h + (i & 3);
-        e[i] = rl[0][m] == place ? ra[0][m] : 0.f;
-        f[i] = e[i] - (float)(__bf16)e[i];
-      }
-      hi[x][0] = pack8(e);
-      hi[x][1] = pack8(e + 8);
-      lo[x][0] = pack8(f);
-      lo[x][1] = pack8(f + 8);
+    for (int i = 0; i < kTile * kHeadGroup / 256; ++i)
+      *reinterpret_cast<float4*>(q + (i * 64 + lane) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (;;) {   // many: the entries of the tile's rows are a run of the list
+      const bool in = b + lane < b1 && (few ? lane < kTile : (en.x & 0xffffffu) / kTile == tile);
+      // (one wave's LDS additions happen in its own order: repeated ids always add up the same way)
+      if (in) unsafeAtomicAdd(q + (few ? lane : en.x % kTile) * kHeadGroup + (en.x >> 24), __uint_as_float(en.y));
+      const int found = __popcll(__builtin_amdgcn_ballot_w64(in));
+      b += found;
+      if (found < 64 || b >= b1) break;
+      en = list[min(b + lane, b1 - 1)];
     }
-    product_o<D>(o, tiles[0], hi);
-    product_o<D>(o, tiles[0], lo);
-    __syncthreads();
+    stream_wait<0>();
+    lds_done();
+#pragma unroll 1
+    for (int rest = 0; rest < 2; ++rest) {
+      bf16x8 p[2][2];
+      coefficients(p, q, rest);
+      product_o<D>(o, own, p);
+    }
   }
 #pragma unroll
   for (int x = 0; x < 2; ++x)
@@ -550,6 +606,7 @@ int head_splits(int64_t rows, int V) {
 template <int D>
 hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   const HeadLayout l = head_layout(a.rows, a.V, a.r, a.teacher.k, a.d_rho != nullptr);
+  const unsigned key_bytes = (unsigned)l.keys * sizeof(uint32_t);
   const bf16_t *rho = (const bf16_t*)a.rho, *W = (const bf16_t*)a.w;
   float2* part_sum = (float2*)a.ws;
   float* part_o = (float*)(a.ws + l.off_o);
@@ -567,7 +624,7 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   o.row = (float2*)(a.ws + l.off_row);
   o.coef = (float*)(a.ws + l.off_coef);
   uint32_t *counts = (uint32_t*)(a.ws + l.off_counts), *totals = (uint32_t*)(a.ws + l.off_totals);
-  uint32_t* begin = totals + l.tiles;
+  uint32_t* begin = totals + l.keys;
   uint2* list = (uint2*)(a.ws + l.off_list);
   const int64_t n = a.rows * a.teacher.k;
   k_head_rho<D, true><<<grid, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher.c, l.splits, part_sum, part_o);
@@ -575,11 +632,13 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   k_head_finish<true><<<(unsigned)a.rows, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher, a.weight, l.splits,
                                                              part_sum, part_o, o);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_sort_count<<<(unsigned)l.chunks, 64, 0, st>>>(a.teacher, n, a.V, l.tiles, l.chunk, counts);
+  k_sort_count<<<(unsigned)l.chunks, 64, key_bytes, st>>>(a.teacher, n, a.V, l.keys, l.chunk, counts);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_sort_scan<<<(unsigned)l.tiles, kThreads, 0, st>>>(counts, l.chunks, l.tiles, totals);
+  k_sort_scan<<<(unsigned)l.keys, kThreads, 0, st>>>(counts, l.chunks, l.keys, totals);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_sort_place<<<(unsigned)l.chunks, 64, 0, st>>>(a.teacher, n, a.V, l.tiles, l.chunk, counts, totals, o.coef, begin, list);
+  k_sort_base<<<1, 1024, 0, st>>>(totals, l.keys, begin);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  k_sort_place<<<(unsigned)l.chunks, 64, key_bytes, st>>>(a.teacher, n, a.V, l.keys, l.chunk, counts, begin, o.coef, list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_head_w<D><<<(unsigned)l.tiles, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher.c, o.row, begin, list,
                                                       (bf16_t*)a.d_w);
@@ -593,6 +652,7 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
   HeadLayout l = {};
   l.splits = head_splits(rows, V);
   l.tiles = (V + kHold - 1) / kHold;
+  l.keys = l.tiles * (kHold / kHeadGroup);   // every wave's, also past V
   const int64_t n = rows * k;
   // chunks of at least 512 entries, at most 1,024 of them
   l.chunk = (int)std::max<int64_t>(512, ((n + 1023) / 1024 + 63) / 64 * 64);
@@ -602,13 +662,13 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
     l.off_o = at;
     at += up((size_t)l.splits * rows * r * sizeof(float));
     l.off_row = at;
-    at += up((size_t)rows * sizeof(float2));
+    at += up((size_t)(rows + kTile) * sizeof(float2));
     l.off_coef = at;
     at += up((size_t)n * sizeof(float));
     l.off_counts = at;
-    at += up((size_t)l.chunks * l.tiles * sizeof(uint32_t));
+    at += up((size_t)l.chunks * l.keys * sizeof(uint32_t));
     l.off_totals = at;
-    at += up(((size_t)2 * l.tiles + 1) * sizeof(uint32_t));
+    at += up(((size_t)2 * l.keys + 1) * sizeof(uint32_t));
     l.off_list = at;
     at += up((size_t)n * sizeof(uint2));
   }

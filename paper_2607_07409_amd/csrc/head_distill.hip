@@ -31,7 +31,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kHold = kHeadTile;      // rows of X per workgroup: 64 per wave
 constexpr int kTile = 32;             // rows of Y per tile
-constexpr float kSlack = 16.f;        // exponents may pass the reference by this before the sums are rescaled
+constexpr float kMostSum = 0x1p20f;   // of a tile's 16 terms in a lane, above which the reference moves
 
 // ------------------------------------------------------------------------------------------
 // tiles
@@ -44,22 +44,22 @@ struct Tile {
   static constexpr int kLoads = kTile * kPieces / kThreads;          // per thread
   bf16_t y[kTile * D];
 };
-constexpr int kBuffers = 3;   // one tile is multiplied, two are on their way
+constexpr int kBuffers = 4;   // a tile in the first product, its predecessor in the second, two on their way
 
-// The streams into LDS bypass the registers: 16 (or 4) bytes a lane from its own address to consecutive places from a
-// wave's LDS address (in M0) on.  The compiler does not count them, so the waits are written out.
+// The streams into LDS bypass the registers: 16 (or 4) bytes a lane from base + its own offset to consecutive places
+// from a wave's LDS address (in M0) on.  The compiler does not count them, so the waits are written out.
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
-__device__ __forceinline__ void stream_to_lds16(const void* from, uint32_t to) {
+__device__ __forceinline__ void stream_to_lds16(const void* base, uint32_t offset, uint32_t to) {
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base) : "memory");
 }
-__device__ __forceinline__ void stream_to_lds4(const void* from, uint32_t to) {
+__device__ __forceinline__ void stream_to_lds4(const void* base, uint32_t offset, uint32_t to) {
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base) : "memory");
 }
 // all but this wave's last n streams have arrived
 template <int n>
@@ -67,16 +67,24 @@ __device__ __forceinline__ void stream_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
 }
 
-// A wave's share of a tile (`row_of(v)` gives the row of Y for tile row v, in range; pieces past r are replaced by
-// the row's first: what they meet in X is 0)
-template <int D, typename RowOf>
-__device__ __forceinline__ void tile_stream(const Tile<D>& to, const bf16_t* Y, int r, RowOf row_of) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+// byte offset of piece g of a row in memory, of row v's place g in LDS; pieces past r are replaced by the row's first
+// (what they meet in X is 0)
+template <int D>
+__device__ __forceinline__ uint32_t piece_offset(uint32_t place, uint32_t v, uint32_t r) {
+  const uint32_t g = place ^ (v & Tile<D>::kSwizzle);
+  return g * 8 < r ? g * 16 : 0;
+}
+// A wave's share of tile number `tile` of Y's rows (those past the last are the last)
+template <int D>
+__device__ __forceinline__ void tile_stream(const Tile<D>& to, const bf16_t* Y, int tile, int64_t rows, uint32_t r) {
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t v0 = threadIdx.x / Tile<D>::kPieces, place = threadIdx.x % Tile<D>::kPieces;
+  const uint32_t most = (uint32_t)min((int64_t)kTile - 1, rows - 1 - (int64_t)tile * kTile);
+  const bf16_t* base = Y + (size_t)tile * kTile * r;
 #pragma unroll
-  for (int q = 0; q < Tile<D>::kLoads; ++q) {
-    const int p0 = (q * kWaves + wave) * 64, p = p0 + lane;
-    const int v = p / Tile<D>::kPieces, g = (p % Tile<D>::kPieces) ^ (v & Tile<D>::kSwizzle);
-    stream_to_lds16(Y + (size_t)row_of(v) * r + (g * 8 < r ? g * 8 : 0), lds_address(to.y) + p0 * 16);
+  for (uint32_t q = 0; q < Tile<D>::kLoads; ++q) {
+    const uint32_t v = v0 + q * (kThreads / Tile<D>::kPieces);
+    stream_to_lds16(base, min(v, most) * (2 * r) + piece_offset<D>(place, v, r), lds_address(to.y) + (q * kWaves + wave) * 1024);
   }
 }
 
@@ -97,18 +105,55 @@ __device__ __forceinline__ void hold_load(bf16x8 (&xf)[2][D / 16], const bf16_t*
   }
 }
 
+// The first product's matrix instructions are written out: their results belong in ordinary registers, where the
+// exponentials read them, while the accumulator registers hold nothing but the second product's sums (for r = 256 all
+// 256 of them).  results_settle: the distance that such a result must keep to the instructions that read it.
+__device__ __forceinline__ void mfma_first(f32x16& d, bf16x8 a, bf16x8 b) {
+  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_add(f32x16& d, bf16x8 a, bf16x8 b) {
+  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void results_settle(f32x16 (&s)[2]) {
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[0]), "+v"(s[1]));
+}
+
 // S^T: tile row m = 8 (i / 4) + 4 half + i % 4 in register i, held row n in the lane
 template <int D>
 __device__ __forceinline__ void product_s(f32x16 (&s)[2], const Tile<D>& t, const bf16x8 (&xf)[2][D / 16]) {
+  constexpr int kAhead = 4;   // pieces read ahead of the products
   const int lane = threadIdx.x & 63, m = lane & 31, h = lane >> 5;
   const char* row = reinterpret_cast<const char*>(t.y) + m * D * 2;
   const int at = (h ^ (m & Tile<D>::kSwizzle)) << 4;
-  s[0] = s[1] = f32x16{};
+  bf16x8 a[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) a[k] = *reinterpret_cast<const bf16x8*>(row + (at ^ (k << 5)));
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
-    const bf16x8 a = *reinterpret_cast<const bf16x8*>(row + (at ^ (k << 5)));
-    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, xf[0][k], s[0], 0, 0, 0);
-    s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, xf[1][k], s[1], 0, 0, 0);
+    if (k == 0) {
+      mfma_first(s[0], a[0], xf[0][0]);
+      mfma_first(s[1], a[0], xf[1][0]);
+    } else {
+      mfma_add(s[0], a[k % kAhead], xf[0][k]);
+      mfma_add(s[1], a[k % kAhead], xf[1][k]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (k + kAhead < D / 16) a[k % kAhead] = *reinterpret_cast<const bf16x8*>(row + (at ^ ((k + kAhead) << 5)));
+  }
+  results_settle(s);
+}
+// hints to the scheduler for the block before them: the second product between the exponentials of the next tile
+template <int D>
+__device__ __forceinline__ void order_o() {
+  constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100;
+  constexpr int kProducts = D / 8;
+  __builtin_amdgcn_sched_group_barrier(kLdsRead, 8, 0);
+#pragma unroll
+  for (int k = 0; k < kProducts; ++k) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kValu, 4 * 32 / kProducts, 0);
+    __builtin_amdgcn_sched_group_barrier(kTrans, 32 / kProducts, 0);
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
   }
 }
 
@@ -170,40 +215,67 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
   const int nt = (V + kTile - 1) / kTile;
   const int t0 = (int)((int64_t)nt * sp / splits), t1 = (int)((int64_t)nt * (sp + 1) / splits);
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  auto row_of = [&](int t) { return [=](int v) { return min(t * kTile + v, V - 1); }; };
 
   bf16x8 xf[2][D / 16];
   hold_load<D>(xf, rho, x0, rows, r);
   f32x16 o[2][GRAD ? D / 32 : 1] = {};
   float ref[2] = {kNoRef, kNoRef}, sum[2] = {0.f, 0.f};
-  tile_stream(tiles[0], W, r, row_of(min(t0, nt - 1)));
-  tile_stream(tiles[1], W, r, row_of(min(t0 + 1, nt - 1)));
-  int at = 0;   // t's buffer
+  tile_stream(tiles[0], W, min(t0, nt - 1), V, r);
+  tile_stream(tiles[1], W, min(t0 + 1, nt - 1), V, r);
+  bf16x8 p[2][2] = {};   // the tile before, whose second product runs beside this one's exponentials
+  int at = 0, before = 0;   // t's buffer and the one before it (at first t's own: p is 0)
   for (int t = t0; t < t1; ++t) {
     stream_wait<Tile<D>::kLoads>();   // t has arrived; t + 1 may be on its way
-    __syncthreads();                  // everybody's share of it, and everybody is done with t - 1
-    const Tile<D>& cur = tiles[at];
-    tile_stream(tiles[at == 0 ? 2 : at - 1], W, r, row_of(min(t + 2, nt - 1)));
-    at = at == 2 ? 0 : at + 1;
+    __syncthreads();                  // everybody's share of it, and everybody is done with t - 2
+    const Tile<D>&cur = tiles[at], &last = tiles[before];
+    tile_stream(tiles[(at + 2) & 3], W, min(t + 2, nt - 1), V, r);
+    before = at;
+    at = (at + 1) & 3;
     f32x16 s[2];
-    product_s<D>(s, cur, xf);
-    if (t == nt - 1) {   // rows of the last tile past V
+    auto tile_logits = [&]() {
+      product_s<D>(s, cur, xf);
+      if (t == nt - 1) {   // rows of the last tile past V
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (t * kTile + 8 * (i >> 2) + 4 * h + (i & 3) >= V) s[0][i] = s[1][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i)
+          if (t * kTile + 8 * (i >> 2) + 4 * h + (i & 3) >= V) s[0][i] = s[1][i] = -INFINITY;
+      }
+    };
+    tile_logits();
+    bf16x8 now[2][2];
+    float add[2];
+    auto exponentials = [&](int x) {
+      add[x] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -ref[x]));
+          add[x] += e[i];
+        }
+        if (GRAD) now[x][j] = pack8(e);
+      }
+    };
+    exponentials(0);
+    exponentials(1);
+    if constexpr (GRAD) {
+      product_o<D>(o, last, p);
+      order_o<D>();
     }
-    bf16x8 p[2][2];
+    // Entries far above the reference (those of the first tile are): a new one, the sums rescaled, the tile again
+    if (__builtin_amdgcn_ballot_w64(!(fmaxf(add[0], add[1]) < kMostSum))) {
+      tile_logits();   // (again, so that they need not be kept)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float top = s[x][0];
+      for (int x = 0; x < 2; ++x) {
+        float top = s[x][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[x][i]);
-      top *= c;
-      if (__builtin_amdgcn_ballot_w64(top > ref[x] + kSlack)) {   // rare after the first tiles
-        const float now = fmaxf(ref[x], fmaxf(top, __shfl_xor(top, 32)));
-        const float f = fast_exp2(fmaxf(ref[x] - now, kNoTerm));
-        ref[x] = now;
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[x][i]);
+        top *= c;
+        const float to = fmaxf(ref[x], fmaxf(top, __shfl_xor(top, 32)));
+        const float f = fast_exp2(fmaxf(ref[x] - to, kNoTerm));
+        ref[x] = to;
         sum[x] *= f;
+        exponentials(x);
         if constexpr (GRAD) {
           acc_settle();
 #pragma unroll
@@ -215,19 +287,16 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
           acc_settle();
         }
       }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -ref[x]));
-          sum[x] += e[i];
-        }
-        if (GRAD) p[x][j] = pack8(e);
-      }
     }
-    if constexpr (GRAD) product_o<D>(o, cur, p);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      sum[x] += add[x];
+      if (GRAD)
+        for (int j = 0; j < 2; ++j) p[x][j] = now[x][j];
+    }
   }
+  if constexpr (GRAD)
+    if (t0 < t1) product_o<D>(o, tiles[before], p);
   stream_wait<0>();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -462,15 +531,14 @@ __global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, in
 // ------------------------------------------------------------------------------------------
 // W held, rho streamed
 // ------------------------------------------------------------------------------------------
-// A wave's own tile of Y, by itself
-template <int D, typename RowOf>
-__device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t* Y, int r, RowOf row_of) {
-  const int lane = threadIdx.x & 63;
+// A wave's own tile of Y, by itself: lane v has the row of tile row v
+template <int D>
+__device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t* Y, uint32_t row, uint32_t r) {
+  const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-  for (int q = 0; q < Tile<D>::kLoads * kWaves; ++q) {
-    const int p = q * 64 + lane;
-    const int v = p / Tile<D>::kPieces, g = (p % Tile<D>::kPieces) ^ (v & Tile<D>::kSwizzle);
-    stream_to_lds16(Y + (size_t)row_of(v) * r + (g * 8 < r ? g * 8 : 0), lds_address(to.y) + q * 1024);
+  for (uint32_t q = 0; q < Tile<D>::kLoads * kWaves; ++q) {
+    const uint32_t v = (q * 64 + lane) / Tile<D>::kPieces, place = (q * 64 + lane) % Tile<D>::kPieces;
+    stream_to_lds16(Y, (uint32_t)__shfl((int)row, (int)v) * (2 * r) + piece_offset<D>(place, v, r), lds_address(to.y) + q * 1024);
   }
 }
 // the left operand of a tile of coefficients q[tile row][held row]: their bf16 values, or what those leave
@@ -499,8 +567,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
                                                         const uint32_t* __restrict__ begin,
                                                         const uint2* __restrict__ list, bf16_t* __restrict__ d_w) {
   // the stream's buffers; after it a tile of each wave
-  static_assert(kBuffers < kWaves, "the waves' own tiles cover the stream's");
-  __shared__ Tile<D> tiles[kWaves];
+  static_assert(kBuffers == kWaves, "the waves' own tiles are the stream's");
+  __shared__ Tile<D> tiles[kBuffers];
   __shared__ float2 stats[kBuffers][kWaves][kTile];   // of a tile's rows, a copy for each wave
   __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients where a group has many entries
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, t = threadIdx.x;
@@ -508,8 +576,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   const int64_t x0 = (int64_t)blockIdx.x * kHold + wave * 64;
   const int nt = (int)((rows + kTile - 1) / kTile);
   auto stream = [&](int tile, int to) {
-    stream_to_lds4((const float*)(row_stats + (size_t)tile * kTile) + lane, lds_address(stats[to][wave]));
-    tile_stream(tiles[to], rho, r, [=](int v) { return (int)min((int64_t)tile * kTile + v, rows - 1); });
+    stream_to_lds4(row_stats + (size_t)tile * kTile, 4 * lane, lds_address(stats[to][wave]));
+    tile_stream(tiles[to], rho, tile, rows, r);
   };
 
   bf16x8 xf[2][D / 16];
@@ -517,17 +585,19 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   f32x16 o[2][D / 32] = {};
   stream(0, 0);
   stream(min(1, nt - 1), 1);
-  int at = 0;
+  bf16x8 p[2][2] = {};   // of the tile before, as in k_head_rho
+  int at = 0, before = 0;
   for (int k = 0; k < nt; ++k) {
     stream_wait<Tile<D>::kLoads + 1>();
     __syncthreads();
-    const Tile<D>& cur = tiles[at];
+    const Tile<D>&cur = tiles[at], &last = tiles[before];
     const float2* st = stats[at][wave];
-    stream(min(k + 2, nt - 1), at == 0 ? 2 : at - 1);
-    at = at == 2 ? 0 : at + 1;
+    stream(min(k + 2, nt - 1), (at + 2) & 3);
+    before = at;
+    at = (at + 1) & 3;
     f32x16 s[2];
     product_s<D>(s, cur, xf);
-    bf16x8 p[2][2];
+    bf16x8 now[2][2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float e[2][8];
@@ -537,11 +607,16 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
 #pragma unroll
         for (int x = 0; x < 2; ++x) e[x][i] = la.y * fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -la.x));
       }
-      p[0][j] = pack8(e[0]);
-      p[1][j] = pack8(e[1]);
+      now[0][j] = pack8(e[0]);
+      now[1][j] = pack8(e[1]);
     }
-    product_o<D>(o, cur, p);
+    product_o<D>(o, last, p);
+    order_o<D>();
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      for (int j = 0; j < 2; ++j) p[x][j] = now[x][j];
   }
+  product_o<D>(o, tiles[before], p);
   stream_wait<0>();
   __syncthreads();
   // The teacher's entries of this wave's 64 rows of W, in order of the row.  Few of them: 32 entries a tile, each with
@@ -554,9 +629,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   for (uint32_t b = b0; b < b1;) {
     uint2 en = list[min(b + lane, b1 - 1)];
     const uint32_t tile = __builtin_amdgcn_readfirstlane(en.x & 0xffffffu) / kTile;
-    const int mine = few ? (int)(en.x & 0xffffffu) : (int)min((int64_t)tile * kTile + n, rows - 1);   // lane m: tile row m's
+    const uint32_t mine = few ? en.x & 0xffffffu : (uint32_t)min((int64_t)tile * kTile + n, rows - 1);   // lane m: tile row m's
     lds_done();
-    wave_tile_stream(own, rho, r, [&](int v) { return __shfl(mine, v); });
+    wave_tile_stream(own, rho, mine, r);
 #pragma unroll
     for (int i = 0; i < kTile * kHeadGroup / 256; ++i)
       *reinterpret_cast<float4*>(q + (i * 64 + lane) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -573,7 +648,6 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
     lds_done();
 #pragma unroll 1
     for (int rest = 0; rest < 2; ++rest) {
-      bf16x8 p[2][2];
       coefficients(p, q, rest);
       product_o<D>(o, own, p);
     }

@@ -44,7 +44,8 @@ struct Tile {
   static constexpr int kLoads = kTile * kPieces / kThreads;          // per thread
   bf16_t y[kTile * D];
 };
-constexpr int kBuffers = 4;   // a tile in the first product, its predecessor in the second, two on their way
+constexpr int kBuffers = 5;   // a tile in the first product, its predecessor in the second, three that arrive
+__device__ __forceinline__ int next_buffer(int b) { return b == kBuffers - 1 ? 0 : b + 1; }
 
 // The streams into LDS bypass the registers: 16 (or 4) bytes a lane from base + its own offset to consecutive places
 // from a wave's LDS address (in M0) on.  The compiler does not count them, so the waits are written out.
@@ -118,16 +119,22 @@ __device__ __forceinline__ void results_settle(f32x16 (&s)[2]) {
   asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[0]), "+v"(s[1]));
 }
 
-// S^T: tile row m = 8 (i / 4) + 4 half + i % 4 in register i, held row n in the lane
+// S^T: tile row m = 8 (i / 4) + 4 half + i % 4 in register i, held row n in the lane.  The tile's first pieces are read
+// beforehand (pieces_first), the others as many products ahead.
+constexpr int kAhead = 4;
 template <int D>
-__device__ __forceinline__ void product_s(f32x16 (&s)[2], const Tile<D>& t, const bf16x8 (&xf)[2][D / 16]) {
-  constexpr int kAhead = 4;   // pieces read ahead of the products
+__device__ __forceinline__ bf16x8 piece(const Tile<D>& t, int k) {
   const int lane = threadIdx.x & 63, m = lane & 31, h = lane >> 5;
-  const char* row = reinterpret_cast<const char*>(t.y) + m * D * 2;
-  const int at = (h ^ (m & Tile<D>::kSwizzle)) << 4;
-  bf16x8 a[kAhead];
+  return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(t.y) + m * D * 2 +
+                                          (((h ^ (m & Tile<D>::kSwizzle)) << 4) ^ (k << 5)));
+}
+template <int D>
+__device__ __forceinline__ void pieces_first(bf16x8 (&a)[kAhead], const Tile<D>& t) {
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) a[k] = *reinterpret_cast<const bf16x8*>(row + (at ^ (k << 5)));
+  for (int k = 0; k < kAhead; ++k) a[k] = piece(t, k);
+}
+template <int D>
+__device__ __forceinline__ void product_s(f32x16 (&s)[2], bf16x8 (&a)[kAhead], const Tile<D>& t, const bf16x8 (&xf)[2][D / 16]) {
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
     if (k == 0) {
@@ -138,57 +145,92 @@ __device__ __forceinline__ void product_s(f32x16 (&s)[2], const Tile<D>& t, cons
       mfma_add(s[1], a[k % kAhead], xf[1][k]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (k + kAhead < D / 16) a[k % kAhead] = *reinterpret_cast<const bf16x8*>(row + (at ^ ((k + kAhead) << 5)));
+    if (k + kAhead < D / 16) a[k % kAhead] = piece(t, k + kAhead);
   }
   results_settle(s);
 }
-// hints to the scheduler for the block before them: the second product between the exponentials of the next tile
+
+// O[held row][d] += P^T Y.  p[x][j]: the registers 8 j .. 8 j + 7 of S^T's layout, that is tile rows
+// 16 j + 8 (e / 4) + 4 half + e % 4; the right operand takes its rows in the same order.  Step q is the pair of products
+// of 32 columns and 16 rows; `beside(q)` follows it, in the time that the products take.
 template <int D>
-__device__ __forceinline__ void order_o() {
-  constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100;
-  constexpr int kProducts = D / 8;
-  __builtin_amdgcn_sched_group_barrier(kLdsRead, 8, 0);
+__device__ __forceinline__ bf16x8 columns(const Tile<D>& t, int q) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const int lane = threadIdx.x & 63, h = lane >> 5, dt = q / 2, j = q % 2;
+  const int v = 4 * h + ((lane & 15) >> 2);                          // + 16 j + 8 e4
+  const int g = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);           // + 4 dt
+  union {
+    s16x4 q[2];
+    bf16x8 b;
+  } y;
 #pragma unroll
-  for (int k = 0; k < kProducts; ++k) {
-    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(kValu, 4 * 32 / kProducts, 0);
-    __builtin_amdgcn_sched_group_barrier(kTrans, 32 / kProducts, 0);
-    __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+  for (int e4 = 0; e4 < 2; ++e4) {
+    const int row = v + 8 * e4;
+    const bf16_t* at = t.y + (row + 16 * j) * D + (((g ^ (row & Tile<D>::kSwizzle)) ^ (4 * dt)) << 3) + 4 * (lane & 1);
+    y.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+  }
+  return y.b;
+}
+template <int D, typename Beside>
+__device__ __forceinline__ void product_o(f32x16 (&o)[2][D / 32], const Tile<D>& t, const bf16x8 (&p)[2][2], Beside beside) {
+  constexpr int kSteps = D / 16, kEarly = 3;
+  bf16x8 y[kEarly];
+#pragma unroll
+  for (int q = 0; q < kEarly; ++q) y[q] = columns(t, q);
+#pragma unroll
+  for (int q = 0; q < kSteps; ++q) {
+    o[0][q / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[0][q % 2], y[q % kEarly], o[0][q / 2], 0, 0, 0);
+    o[1][q / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[1][q % 2], y[q % kEarly], o[1][q / 2], 0, 0, 0);
+    if (q + kEarly < kSteps) y[q % kEarly] = columns(t, q + kEarly);
+    beside(q);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// O[held row][d] += P^T Y.  p[x][j]: the registers 8 j .. 8 j + 7 of S^T's layout, that is tile rows
-// 16 j + 8 (e / 4) + 4 half + e % 4; the right operand takes its rows in the same order.
+// The probabilities of a tile from its logits, a few at a step of the tile before's second product: `begin(x, i)` is
+// the exponential of register i, `end(x, i, e)` its value, a step later.
 template <int D>
-__device__ __forceinline__ void product_o(f32x16 (&o)[2][D / 32], const Tile<D>& t, const bf16x8 (&p)[2][2]) {
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-  const int v = 4 * h + ((lane & 15) >> 2);                          // + 16 j + 8 e4
-  const int g = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);           // + 4 dt
+struct Exponentials {
+  static constexpr int kPer = 256 / D;   // registers a step
+  float e[2][16];
+  template <typename Begin, typename End>
+  __device__ __forceinline__ void step(int q, Begin begin, End end) {
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) {
+    for (int i = q * kPer; i < (q + 1) * kPer; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      union {
-        s16x4 q[2];
-        bf16x8 b;
-      } y;
-#pragma unroll
-      for (int e4 = 0; e4 < 2; ++e4) {
-        const int row = v + 8 * e4;
-        const bf16_t* at = t.y + (row + 16 * j) * D + (((g ^ (row & Tile<D>::kSwizzle)) ^ (4 * dt)) << 3) + 4 * (lane & 1);
-        y.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      }
-      o[0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[0][j], y.b, o[0][dt], 0, 0, 0);
-      o[1][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[1][j], y.b, o[1][dt], 0, 0, 0);
-    }
+      for (int x = 0; x < 2; ++x) e[x][i] = begin(x, i);
+    if (q > 0) finish(q - 1, end);
   }
-}
+  template <typename End>
+  __device__ __forceinline__ void finish(int q, End end) {
+#pragma unroll
+    for (int i = q * kPer; i < (q + 1) * kPer; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) e[x][i] = end(x, i, e[x][i]);
+  }
+};
 
 __device__ __forceinline__ bf16x8 pack8(const float* v) {
   const f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
   return __builtin_convertvector(f, bf16x8);
 }
+
+// two probabilities as a word of an operand
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+struct Words {
+  uint32_t w[2][8];
+  __device__ __forceinline__ void operand(bf16x8 (&p)[2][2]) const {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        p[x][j] = __builtin_bit_cast(bf16x8, uint4{w[x][4 * j], w[x][4 * j + 1], w[x][4 * j + 2], w[x][4 * j + 3]});
+  }
+};
 
 // An accumulator register times f, in place: written out so that the sums stay in the accumulator registers also where
 // they are rescaled (the compiler moves all of them out and back in every tile otherwise).  acc_settle covers the
@@ -220,51 +262,53 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
   hold_load<D>(xf, rho, x0, rows, r);
   f32x16 o[2][GRAD ? D / 32 : 1] = {};
   float ref[2] = {kNoRef, kNoRef}, sum[2] = {0.f, 0.f};
-  tile_stream(tiles[0], W, min(t0, nt - 1), V, r);
-  tile_stream(tiles[1], W, min(t0 + 1, nt - 1), V, r);
-  bf16x8 p[2][2] = {};   // the tile before, whose second product runs beside this one's exponentials
-  int at = 0, before = 0;   // t's buffer and the one before it (at first t's own: p is 0)
+  constexpr int kLoads = Tile<D>::kLoads;
+  for (int i = 0; i < 3; ++i) tile_stream(tiles[i], W, min(t0 + i, nt - 1), V, r);
+  stream_wait<2 * kLoads>();
+  __syncthreads();
+  bf16x8 a[kAhead], p[2][2] = {};   // p: of the tile before, whose second product runs beside this one's exponentials
+  pieces_first(a, tiles[0]);
+  int at = 0, before = 0;           // t's buffer and the one before it (at first t's own: p is 0)
   for (int t = t0; t < t1; ++t) {
-    stream_wait<Tile<D>::kLoads>();   // t has arrived; t + 1 may be on its way
-    __syncthreads();                  // everybody's share of it, and everybody is done with t - 2
     const Tile<D>&cur = tiles[at], &last = tiles[before];
-    tile_stream(tiles[(at + 2) & 3], W, min(t + 2, nt - 1), V, r);
-    before = at;
-    at = (at + 1) & 3;
+    const int next = next_buffer(at), free = next_buffer(next_buffer(next));
     f32x16 s[2];
-    auto tile_logits = [&]() {
-      product_s<D>(s, cur, xf);
-      if (t == nt - 1) {   // rows of the last tile past V
+    auto past_v = [&]() {   // rows of the last tile past V
+      if (t == nt - 1)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (t * kTile + 8 * (i >> 2) + 4 * h + (i & 3) >= V) s[0][i] = s[1][i] = -INFINITY;
-      }
     };
-    tile_logits();
-    bf16x8 now[2][2];
-    float add[2];
-    auto exponentials = [&](int x) {
-      add[x] = 0.f;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -ref[x]));
-          add[x] += e[i];
-        }
-        if (GRAD) now[x][j] = pack8(e);
-      }
+    product_s<D>(s, a, cur, xf);
+    past_v();
+    stream_wait<kLoads>();   // t + 1 has arrived, t + 2 may be on its way
+    __syncthreads();         // everybody's share of it, and everybody is done with t - 2: its buffer takes t + 3
+    float add[2] = {0.f, 0.f};
+    Exponentials<D> ex;
+    Words now;
+    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -ref[x])); };
+    auto end = [&](int x, int i, float e) {
+      add[x] += e;
+      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], e);
+      return e;
     };
-    exponentials(0);
-    exponentials(1);
     if constexpr (GRAD) {
-      product_o<D>(o, last, p);
-      order_o<D>();
+      product_o<D>(o, last, p, [&](int q) {
+        if (q == 0) tile_stream(tiles[free], W, min(t + 3, nt - 1), V, r);
+        ex.step(q, begin, end);
+      });
+    } else {
+      tile_stream(tiles[free], W, min(t + 3, nt - 1), V, r);
+#pragma unroll
+      for (int q = 0; q < D / 16; ++q) ex.step(q, begin, end);
     }
+    pieces_first(a, tiles[next]);
+    ex.finish(D / 16 - 1, end);
     // Entries far above the reference (those of the first tile are): a new one, the sums rescaled, the tile again
     if (__builtin_amdgcn_ballot_w64(!(fmaxf(add[0], add[1]) < kMostSum))) {
-      tile_logits();   // (again, so that they need not be kept)
+      pieces_first(a, cur);
+      product_s<D>(s, a, cur, xf);   // (so that the logits need not be kept)
+      past_v();
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         float top = s[x][0];
@@ -275,7 +319,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
         const float f = fast_exp2(fmaxf(ref[x] - to, kNoTerm));
         ref[x] = to;
         sum[x] *= f;
-        exponentials(x);
+        add[x] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ex.e[x][i] = end(x, i, begin(x, i));
         if constexpr (GRAD) {
           acc_settle();
 #pragma unroll
@@ -287,16 +333,16 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
           acc_settle();
         }
       }
+      pieces_first(a, tiles[next]);
     }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      sum[x] += add[x];
-      if (GRAD)
-        for (int j = 0; j < 2; ++j) p[x][j] = now[x][j];
-    }
+    sum[0] += add[0];
+    sum[1] += add[1];
+    if (GRAD) now.operand(p);
+    before = at;
+    at = next;
   }
   if constexpr (GRAD)
-    if (t0 < t1) product_o<D>(o, tiles[before], p);
+    if (t0 < t1) product_o<D>(o, tiles[before], p, [](int) {});
   stream_wait<0>();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -567,7 +613,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
                                                         const uint32_t* __restrict__ begin,
                                                         const uint2* __restrict__ list, bf16_t* __restrict__ d_w) {
   // the stream's buffers; after it a tile of each wave
-  static_assert(kBuffers == kWaves, "the waves' own tiles are the stream's");
+  static_assert(kBuffers >= kWaves, "the stream's buffers hold the waves' own tiles");
   __shared__ Tile<D> tiles[kBuffers];
   __shared__ float2 stats[kBuffers][kWaves][kTile];   // of a tile's rows, a copy for each wave
   __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients where a group has many entries
@@ -583,40 +629,40 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   bf16x8 xf[2][D / 16];
   hold_load<D>(xf, W, x0, V, r);
   f32x16 o[2][D / 32] = {};
-  stream(0, 0);
-  stream(min(1, nt - 1), 1);
-  bf16x8 p[2][2] = {};   // of the tile before, as in k_head_rho
+  constexpr int kLoads = Tile<D>::kLoads + 1;
+  for (int i = 0; i < 3; ++i) stream(min(i, nt - 1), i);
+  stream_wait<2 * kLoads>();
+  __syncthreads();
+  bf16x8 a[kAhead], p[2][2] = {};   // as in k_head_rho
+  pieces_first(a, tiles[0]);
   int at = 0, before = 0;
   for (int k = 0; k < nt; ++k) {
-    stream_wait<Tile<D>::kLoads + 1>();
-    __syncthreads();
-    const Tile<D>&cur = tiles[at], &last = tiles[before];
+    const int next = next_buffer(at), free = next_buffer(next_buffer(next));
     const float2* st = stats[at][wave];
-    stream(min(k + 2, nt - 1), (at + 2) & 3);
-    before = at;
-    at = (at + 1) & 3;
     f32x16 s[2];
-    product_s<D>(s, cur, xf);
-    bf16x8 now[2][2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float e[2][8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 la = st[16 * j + 8 * (i >> 2) + 4 * h + (i & 3)];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) e[x][i] = la.y * fast_exp2(__builtin_fmaf(s[x][8 * j + i], c, -la.x));
-      }
-      now[0][j] = pack8(e[0]);
-      now[1][j] = pack8(e[1]);
-    }
-    product_o<D>(o, last, p);
-    order_o<D>();
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-      for (int j = 0; j < 2; ++j) p[x][j] = now[x][j];
+    product_s<D>(s, a, tiles[at], xf);
+    stream_wait<kLoads>();
+    __syncthreads();
+    Exponentials<D> ex;
+    Words now;
+    auto stat = [&](int i) { return st[8 * (i >> 2) + 4 * h + (i & 3)]; };
+    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -stat(i).x)); };
+    auto end = [&](int x, int i, float e) {
+      e *= stat(i).y;
+      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], e);
+      return e;
+    };
+    product_o<D>(o, tiles[before], p, [&](int q) {
+      if (q == 0) stream(min(k + 3, nt - 1), free);
+      ex.step(q, begin, end);
+    });
+    pieces_first(a, tiles[next]);
+    ex.finish(D / 16 - 1, end);
+    now.operand(p);
+    before = at;
+    at = next;
   }
-  product_o<D>(o, tiles[before], p);
+  product_o<D>(o, tiles[before], p, [](int) {});
   stream_wait<0>();
   __syncthreads();
   // The teacher's entries of this wave's 64 rows of W, in order of the row.  Few of them: 32 entries a tile, each with
@@ -649,7 +695,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
 #pragma unroll 1
     for (int rest = 0; rest < 2; ++rest) {
       coefficients(p, q, rest);
-      product_o<D>(o, own, p);
+      product_o<D>(o, own, p, [](int) {});
     }
   }
 #pragma unroll

@@ -36,13 +36,22 @@ constexpr float kMostSum = 0x1p20f;   // of a tile's 16 terms in a lane, above w
 // ------------------------------------------------------------------------------------------
 // tiles
 // ------------------------------------------------------------------------------------------
-// Y tile in LDS: row v of D bf16, its 16-byte piece g at place g ^ (v & swizzle)
+// Y tile in LDS, in 16-byte pieces: four rows together, of each 64 bytes in turn, and within those the four pieces
+// permuted by the next two bits of the row.  So one piece of 16 successive rows (a read of the first product) covers 256
+// bytes, four pieces of four successive rows (a transposed read of the second) as well, and every read of a tile is at
+// a constant distance from one or two addresses of its lane.
 template <int D>
 struct Tile {
   static constexpr int kPieces = D / 8;                              // per row
-  static constexpr int kSwizzle = (kPieces < 16 ? kPieces : 16) - 1;
   static constexpr int kLoads = kTile * kPieces / kThreads;          // per thread
+  static constexpr int kQuad = 4 * D;                                // elements of four rows
   bf16_t y[kTile * D];
+  // row and piece at a place
+  __device__ __forceinline__ static void at(uint32_t place, uint32_t* row, uint32_t* piece) {
+    const uint32_t quad = place / (kQuad / 8), in = place % (kQuad / 8);
+    *row = quad * 4 + in / 4 % 4;
+    *piece = in / 16 * 4 + ((in ^ quad) & 3);
+  }
 };
 constexpr int kBuffers = 5;   // a tile in the first product, its predecessor in the second, three that arrive
 __device__ __forceinline__ int next_buffer(int b) { return b == kBuffers - 1 ? 0 : b + 1; }
@@ -52,10 +61,26 @@ __device__ __forceinline__ int next_buffer(int b) { return b == kBuffers - 1 ? 0
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
-__device__ __forceinline__ void stream_to_lds16(const void* base, uint32_t offset, uint32_t to) {
+// N times 16 bytes a lane, to N successive KiB; offset q is that of the q-th plus (N - 1 - q) KiB.  (An instruction's
+// immediate offset counts on both sides; the base is taken N - 1 KiB lower.)
+template <int N>
+__device__ __forceinline__ void stream_to_lds16(const void* from, const uint32_t (&offset)[N], uint32_t to) {
+  static_assert(N == 1 || N == 2 || N == 4, "tiles of rank 64, 128 and 256");
+  const char* base = (const char*)from - (N - 1) * 1024;
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base) : "memory");
+  to = __builtin_amdgcn_readfirstlane(to);
+  if constexpr (N == 1)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(to), "s"(base), "v"(offset[0]) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                 "global_load_lds_dwordx4 %4, %2 offset:1024\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(to), "s"(base), "v"(offset[0]), "v"(offset[1]) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                 "global_load_lds_dwordx4 %4, %2 offset:1024\n\tglobal_load_lds_dwordx4 %5, %2 offset:2048\n\t"
+                 "global_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(to), "s"(base), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]) : "memory");
 }
 __device__ __forceinline__ void stream_to_lds4(const void* base, uint32_t offset, uint32_t to) {
   uint32_t m0;
@@ -68,26 +93,36 @@ __device__ __forceinline__ void stream_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
 }
 
-// byte offset of piece g of a row in memory, of row v's place g in LDS; pieces past r are replaced by the row's first
-// (what they meet in X is 0)
+// byte offset of a row's piece in memory; pieces past r are replaced by the row's first (what they meet in X is 0)
+__device__ __forceinline__ uint32_t piece_offset(uint32_t piece, uint32_t r) { return piece * 8 < r ? piece * 16 : 0; }
+// Tiles of the rows 0 .. rows - 1 of Y, each wave its share.  The last of several tiles ends with the last row (it begins
+// with rows of the one before); a single tile of fewer rows repeats the last one.
 template <int D>
-__device__ __forceinline__ uint32_t piece_offset(uint32_t place, uint32_t v, uint32_t r) {
-  const uint32_t g = place ^ (v & Tile<D>::kSwizzle);
-  return g * 8 < r ? g * 16 : 0;
-}
-// A wave's share of tile number `tile` of Y's rows (those past the last are the last)
-template <int D>
-__device__ __forceinline__ void tile_stream(const Tile<D>& to, const bf16_t* Y, int tile, int64_t rows, uint32_t r) {
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t v0 = threadIdx.x / Tile<D>::kPieces, place = threadIdx.x % Tile<D>::kPieces;
-  const uint32_t most = (uint32_t)min((int64_t)kTile - 1, rows - 1 - (int64_t)tile * kTile);
-  const bf16_t* base = Y + (size_t)tile * kTile * r;
+struct TileStream {
+  static constexpr int N = Tile<D>::kLoads;
+  const bf16_t* Y;
+  int64_t rows;
+  uint32_t r, place;   // bytes from a tile to this wave's share
+  uint32_t offset[N];
+  __device__ __forceinline__ TileStream(const bf16_t* Y, int64_t rows, uint32_t r) : Y(Y), rows(rows), r(r) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    place = wave * N * 1024;
 #pragma unroll
-  for (uint32_t q = 0; q < Tile<D>::kLoads; ++q) {
-    const uint32_t v = v0 + q * (kThreads / Tile<D>::kPieces);
-    stream_to_lds16(base, min(v, most) * (2 * r) + piece_offset<D>(place, v, r), lds_address(to.y) + (q * kWaves + wave) * 1024);
+    for (uint32_t q = 0; q < N; ++q) {
+      uint32_t v, g;
+      Tile<D>::at((wave * N + q) * 64 + lane, &v, &g);
+      offset[q] = (uint32_t)min((int64_t)v, rows - 1) * (2 * r) + piece_offset(g, r) + (N - 1 - q) * 1024;
+    }
   }
-}
+  __device__ __forceinline__ static int count(int64_t rows) { return (int)((rows + kTile - 1) / kTile); }
+  // the first row of a tile
+  __device__ __forceinline__ static int64_t first(int tile, int64_t rows) {
+    return min((int64_t)tile * kTile, max(rows - kTile, (int64_t)0));
+  }
+  __device__ __forceinline__ void start(const Tile<D>& to, int tile) const {
+    stream_to_lds16(Y + (size_t)first(tile, rows) * r, offset, lds_address(to.y) + place);
+  }
+};
 
 // the held operand: lane n of tile x has row x0 + 32 x + n, 8 of every 16 columns by its half
 template <int D>
@@ -125,8 +160,8 @@ constexpr int kAhead = 4;
 template <int D>
 __device__ __forceinline__ bf16x8 piece(const Tile<D>& t, int k) {
   const int lane = threadIdx.x & 63, m = lane & 31, h = lane >> 5;
-  return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(t.y) + m * D * 2 +
-                                          (((h ^ (m & Tile<D>::kSwizzle)) << 4) ^ (k << 5)));
+  const int from = (m / 4) * Tile<D>::kQuad + m % 4 * 32 + ((2 * (k & 1) + h) ^ (m / 4 & 3)) * 8;
+  return *reinterpret_cast<const bf16x8*>(t.y + from + (k / 2) * 128);
 }
 template <int D>
 __device__ __forceinline__ void pieces_first(bf16x8 (&a)[kAhead], const Tile<D>& t) {
@@ -157,7 +192,7 @@ template <int D>
 __device__ __forceinline__ bf16x8 columns(const Tile<D>& t, int q) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
   const int lane = threadIdx.x & 63, h = lane >> 5, dt = q / 2, j = q % 2;
-  const int v = 4 * h + ((lane & 15) >> 2);                          // + 16 j + 8 e4
+  const int v = (lane & 15) >> 2;                                    // + 4 h + 16 j + 8 e4
   const int g = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);           // + 4 dt
   union {
     s16x4 q[2];
@@ -165,8 +200,8 @@ __device__ __forceinline__ bf16x8 columns(const Tile<D>& t, int q) {
   } y;
 #pragma unroll
   for (int e4 = 0; e4 < 2; ++e4) {
-    const int row = v + 8 * e4;
-    const bf16_t* at = t.y + (row + 16 * j) * D + (((g ^ (row & Tile<D>::kSwizzle)) ^ (4 * dt)) << 3) + 4 * (lane & 1);
+    const bf16_t* from = t.y + h * Tile<D>::kQuad + v * 32 + (g ^ (h + 2 * e4)) * 8 + 4 * (lane & 1);
+    const bf16_t* at = from + (4 * j + 2 * e4) * Tile<D>::kQuad + dt * 128;
     y.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
   }
   return y.b;
@@ -254,7 +289,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
   __shared__ Tile<D> tiles[kBuffers];
   const int sp = blockIdx.x % splits;
   const int64_t x0 = (int64_t)(blockIdx.x / splits) * kHold + (threadIdx.x >> 6) * 64;
-  const int nt = (V + kTile - 1) / kTile;
+  const int nt = TileStream<D>::count(V);
   const int t0 = (int)((int64_t)nt * sp / splits), t1 = (int)((int64_t)nt * (sp + 1) / splits);
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
 
@@ -263,7 +298,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
   f32x16 o[2][GRAD ? D / 32 : 1] = {};
   float ref[2] = {kNoRef, kNoRef}, sum[2] = {0.f, 0.f};
   constexpr int kLoads = Tile<D>::kLoads;
-  for (int i = 0; i < 3; ++i) tile_stream(tiles[i], W, min(t0 + i, nt - 1), V, r);
+  const TileStream<D> stream(W, V, r);
+  for (int i = 0; i < 3; ++i) stream.start(tiles[i], min(t0 + i, nt - 1));
   stream_wait<2 * kLoads>();
   __syncthreads();
   bf16x8 a[kAhead], p[2][2] = {};   // p: of the tile before, whose second product runs beside this one's exponentials
@@ -273,11 +309,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
     const Tile<D>&cur = tiles[at], &last = tiles[before];
     const int next = next_buffer(at), free = next_buffer(next_buffer(next));
     f32x16 s[2];
-    auto past_v = [&]() {   // rows of the last tile past V
+    auto past_v = [&]() {   // what the last tile repeats
       if (t == nt - 1)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t * kTile + 8 * (i >> 2) + 4 * h + (i & 3) >= V) s[0][i] = s[1][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int v = (int)TileStream<D>::first(t, V) + 8 * (i >> 2) + 4 * h + (i & 3);
+          if (v < t * kTile || v >= V) s[0][i] = s[1][i] = -INFINITY;
+        }
     };
     product_s<D>(s, a, cur, xf);
     past_v();
@@ -294,11 +332,11 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
     };
     if constexpr (GRAD) {
       product_o<D>(o, last, p, [&](int q) {
-        if (q == 0) tile_stream(tiles[free], W, min(t + 3, nt - 1), V, r);
+        if (q == 0) stream.start(tiles[free], min(t + 3, nt - 1));
         ex.step(q, begin, end);
       });
     } else {
-      tile_stream(tiles[free], W, min(t + 3, nt - 1), V, r);
+      stream.start(tiles[free], min(t + 3, nt - 1));
 #pragma unroll
       for (int q = 0; q < D / 16; ++q) ex.step(q, begin, end);
     }
@@ -369,7 +407,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
 struct HeadOut {
   float *loss, *lse;       // either may be NULL
   bf16_t* d_rho;           // with gradients: [rows, r]
-  float2* row;             //   (R + log2 s, g M / T) of each row, to a whole tile of rows
+  float2* row;             //   (R + log2 s, g M / T) in the order of k_head_w's tiles
   float* coef;             //   [rows, K]: -g q_k / T of each entry
 };
 
@@ -443,11 +481,15 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
   if (t == 0) {
     if (o.loss) o.loss[row] = (loss[0] + loss[1]) + (loss[2] + loss[3]);
     if (o.lse) o.lse[row] = row_lse(a);
-    if (GRAD) o.row[row] = make_float2(a.R + l2, w * mass);
+    if (GRAD) {   // the last of several tiles ends with the last row
+      const int64_t whole = rows / kTile * kTile, pad = rows > kTile && rows > whole ? whole + kTile - rows : 0;
+      o.row[row < whole ? row : row + pad] = make_float2(a.R + l2, w * mass);
+    }
   }
   if (GRAD) {
-    // no row: 2^-kMostY times 0
-    if (row == rows - 1 && t > 0 && t < kTile && (row + t) / kTile == row / kTile) o.row[row + t] = make_float2(kMostY, 0.f);
+    // the places of its tile that no row has: 2^-kMostY times 0
+    const int64_t whole = rows / kTile * kTile, left = rows - whole;
+    if (row == rows - 1 && left > 0 && t < kTile - left) o.row[rows > kTile ? whole + t : rows + t] = make_float2(kMostY, 0.f);
     if (t < te.k) o.coef[(size_t)row * te.k + t] = -w * e.q;
     if (wave == 0 && on) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -580,11 +622,18 @@ __global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, in
 // A wave's own tile of Y, by itself: lane v has the row of tile row v
 template <int D>
 __device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t* Y, uint32_t row, uint32_t r) {
+  constexpr int N = Tile<D>::kLoads;
   const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-  for (uint32_t q = 0; q < Tile<D>::kLoads * kWaves; ++q) {
-    const uint32_t v = (q * 64 + lane) / Tile<D>::kPieces, place = (q * 64 + lane) % Tile<D>::kPieces;
-    stream_to_lds16(Y, (uint32_t)__shfl((int)row, (int)v) * (2 * r) + piece_offset<D>(place, v, r), lds_address(to.y) + q * 1024);
+  for (uint32_t w = 0; w < kWaves; ++w) {
+    uint32_t offset[N];
+#pragma unroll
+    for (uint32_t q = 0; q < N; ++q) {
+      uint32_t v, g;
+      Tile<D>::at((w * N + q) * 64 + lane, &v, &g);
+      offset[q] = (uint32_t)__shfl((int)row, (int)v) * (2 * r) + piece_offset(g, r) + (N - 1 - q) * 1024;
+    }
+    stream_to_lds16(Y, offset, lds_address(to.y) + w * N * 1024);
   }
 }
 // the left operand of a tile of coefficients q[tile row][held row]: their bf16 values, or what those leave
@@ -620,10 +669,11 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, t = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t x0 = (int64_t)blockIdx.x * kHold + wave * 64;
-  const int nt = (int)((rows + kTile - 1) / kTile);
+  const int nt = TileStream<D>::count(rows);
+  const TileStream<D> rho_tiles(rho, rows, r);
   auto stream = [&](int tile, int to) {
     stream_to_lds4(row_stats + (size_t)tile * kTile, 4 * lane, lds_address(stats[to][wave]));
-    tile_stream(tiles[to], rho, tile, rows, r);
+    rho_tiles.start(tiles[to], tile);
   };
 
   bf16x8 xf[2][D / 16];

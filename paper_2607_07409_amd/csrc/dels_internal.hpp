@@ -126,6 +126,7 @@ hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t st);
 constexpr int kHeadTile = 256;         // vocabulary entries of a workgroup of the weight gradient
 constexpr int kHeadGroup = 64;         // of a wave
 constexpr int kHeadMostV = 1 << 20;
+constexpr int kHeadMostSplits = 512;   // of the vocabulary
 constexpr int kHeadMostKeys = kHeadMostV / kHeadGroup;
 struct HeadDistillArgs {
   const void *rho, *w;       // bf16 [rows, r], [V, r]
@@ -139,7 +140,8 @@ struct HeadDistillArgs {
 };
 struct HeadLayout {
   int splits;                // of the vocabulary, where rho is held
-  int tiles;                 // of the vocabulary, where W is held
+  int tiles;                 // of the vocabulary, where W is held: `whole` by a workgroup each, the others by
+  int whole, row_splits;     // row_splits workgroups
   int keys, chunk, chunks;   // of the counting sort of the teacher's entries
   size_t off_o, off_row, off_coef, off_counts, off_totals, off_list, total;
 };

@@ -17,6 +17,8 @@
 // rows directly, in float32.  Their part of d_W is summed in k_head_w: the entries are put in order of the vocabulary
 // tile by a stable counting sort (so the sum's order, and every bit, is the same in every run) and streamed after the
 // rows as further tiles of Y, with their coefficients as two bf16 terms.
+#include <type_traits>
+
 #include "teacher.hpp"
 
 namespace dls {
@@ -415,6 +417,27 @@ __device__ __forceinline__ float4 widen4(uint2 v) {
   return make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
 }
 
+// sum over the 64 lanes, in every lane, without the LDS
+__device__ __forceinline__ float wave_total(float v) {
+  auto dpp = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  v += dpp(std::integral_constant<int, 0xB1>{});    // lane ^ 1
+  v += dpp(std::integral_constant<int, 0x4E>{});    // lane ^ 2
+  v += dpp(std::integral_constant<int, 0x141>{});   // the other half of eight
+  v += dpp(std::integral_constant<int, 0x140>{});   // the other half of sixteen
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ void add4(float4& d, float f, float4 y) {
+  d.x = __builtin_fmaf(f, y.x, d.x);
+  d.y = __builtin_fmaf(f, y.y, d.y);
+  d.z = __builtin_fmaf(f, y.z, d.z);
+  d.w = __builtin_fmaf(f, y.w, d.w);
+}
+
 // one workgroup per row: joins the splits, takes the teacher's logits from W, finishes d_rho
 template <bool GRAD>
 __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
@@ -424,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
                                                           const float* __restrict__ part_o, HeadOut o) {
   __shared__ RowShared shr;
   __shared__ TeacherShared sht;
-  __shared__ float q[256], log_q[256], scale[256];
+  __shared__ float q[256], log_q[256], scale[kHeadMostSplits];
   __shared__ int id[256];
   __shared__ float4 acc[kWaves][64];
   __shared__ float loss[kWaves];
@@ -436,44 +459,55 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
   log_q[t] = e.log_q;
   id[t] = e.id;
   RowSum a = row_empty();
-  if (t < splits) {   // splits <= 256
-    const float2 p = part_sum[(size_t)t * rows + row];
-    a.R = p.x;
-    a.s = p.y;
+  for (int i = t; i < splits; i += kThreads) {   // (at most kHeadMostSplits)
+    const float2 p = part_sum[(size_t)i * rows + row];
+    scale[i] = p.x;
+    a = row_merge<false>(a, RowSum{p.x, p.y, 0.f});
   }
-  const float mine = a.R;
   a = row_block_merge<false>(a, shr);
   const float l2 = fast_log2(a.s), w = (weight ? weight[row] : 1.f) * te.inv_temp;
-  scale[t] = t < splits ? w * mass * fast_exp2(fmaxf(mine - a.R, kNoTerm)) / a.s : 0.f;
+  for (int i = t; i < splits; i += kThreads) scale[i] = w * mass * fast_exp2(fmaxf(scale[i] - a.R, kNoTerm)) / a.s;
   __syncthreads();
 
   const bool on = 4 * lane < r;   // this lane's four columns
   const float4 x = on ? widen4(*reinterpret_cast<const uint2*>(rho + (size_t)row * r + 4 * lane)) : make_float4(0, 0, 0, 0);
   float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
   float term = 0.f;
-  for (int k = wave; k < te.k; k += kWaves) {
-    if (id[k] < 0) continue;   // the same for the whole wave
-    const float4 y = on ? widen4(*reinterpret_cast<const uint2*>(W + (size_t)id[k] * r + 4 * lane)) : make_float4(0, 0, 0, 0);
-    const float s = wave_sum(__builtin_fmaf(x.x, y.x, x.y * y.y) + __builtin_fmaf(x.z, y.z, x.w * y.w));
-    const TeacherEntry ek = {id[k], q[k], log_q[k]};
-    term += teacher_term(ek, __builtin_fmaf(s, te.c, -a.R) - l2);
-    if (GRAD) {
-      const float f = -w * q[k];
-      d.x = __builtin_fmaf(f, y.x, d.x);
-      d.y = __builtin_fmaf(f, y.y, d.y);
-      d.z = __builtin_fmaf(f, y.z, d.z);
-      d.w = __builtin_fmaf(f, y.w, d.w);
+  // the wave's entries and splits, four at a time: their loads in flight together
+  for (int k0 = wave; k0 < te.k; k0 += 4 * kWaves) {
+    float4 y[4];
+    float dot[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * kWaves, v = k < te.k ? id[k] : -1;
+      y[u] = on && v >= 0 ? widen4(*reinterpret_cast<const uint2*>(W + (size_t)v * r + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      dot[u] = __builtin_fmaf(x.x, y[u].x, x.y * y[u].y) + __builtin_fmaf(x.z, y[u].z, x.w * y[u].w);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) dot[u] = wave_total(dot[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * kWaves;
+      if (k >= te.k) break;
+      const TeacherEntry ek = {id[k], q[k], log_q[k]};   // (an absent entry's weight is 0)
+      term += teacher_term(ek, __builtin_fmaf(dot[u], te.c, -a.R) - l2);
+      if (GRAD) add4(d, -w * q[k], y[u]);
     }
   }
   if (GRAD && on) {
-    for (int sp = wave; sp < splits; sp += kWaves) {
-      const float4 y = *reinterpret_cast<const float4*>(part_o + ((size_t)sp * rows + row) * r + 4 * lane);
-      const float f = scale[sp];
-      d.x = __builtin_fmaf(f, y.x, d.x);
-      d.y = __builtin_fmaf(f, y.y, d.y);
-      d.z = __builtin_fmaf(f, y.z, d.z);
-      d.w = __builtin_fmaf(f, y.w, d.w);
+    const float* from = part_o + (size_t)row * r + 4 * lane;
+    const size_t step = (size_t)rows * r;
+    int sp = wave;
+    for (; sp + 3 * kWaves < splits; sp += 4 * kWaves) {
+      float4 y[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const float4*>(from + (sp + u * kWaves) * step);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add4(d, scale[sp + u * kWaves], y[u]);
     }
+    for (; sp < splits; sp += kWaves) add4(d, scale[sp], *reinterpret_cast<const float4*>(from + sp * step));
   }
   if (lane == 0) loss[wave] = term;
   if (GRAD) acc[wave][lane] = d;
@@ -636,21 +670,31 @@ __device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t
     stream_to_lds16(Y, offset, lds_address(to.y) + w * N * 1024);
   }
 }
-// the left operand of a tile of coefficients q[tile row][held row]: their bf16 values, or what those leave
-__device__ __forceinline__ void coefficients(bf16x8 (&p)[2][2], const float* q, bool rest) {
+// O += q^T Y for a tile's coefficients q[tile row][held row] in LDS, as two bf16 terms: their rounded values and the rest
+template <int D>
+__device__ __forceinline__ void coefficient_products(f32x16 (&o)[2][D / 32], const Tile<D>& t, const float* q) {
   const int n = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
+  bf16x8 p[2][2][2];
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      float e[8];
+      float e[8], rest[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         e[i] = q[(16 * j + 8 * (i >> 2) + 4 * h + (i & 3)) * kHeadGroup + 32 * x + n];
-        if (rest) e[i] -= (float)(__bf16)e[i];
+        rest[i] = e[i] - (float)(__bf16)e[i];
       }
-      p[x][j] = pack8(e);
+      p[0][x][j] = pack8(e);
+      p[1][x][j] = pack8(rest);
     }
+#pragma unroll 1
+  for (int term = 0; term < 2; ++term) {
+    product_o<D>(o, t, p[0], [](int) {});
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      for (int j = 0; j < 2; ++j) p[0][x][j] = p[1][x][j];
+  }
 }
 // this wave's LDS accesses are done (its next stream may overwrite what they read)
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -660,16 +704,23 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
                                                         int64_t rows, int V, int r, float c,
                                                         const float2* __restrict__ row_stats,
                                                         const uint32_t* __restrict__ begin,
-                                                        const uint2* __restrict__ list, bf16_t* __restrict__ d_w) {
+                                                        const uint2* __restrict__ list, int whole, int splits,
+                                                        bf16_t* __restrict__ d_w, float* __restrict__ part_w) {
+  // the first `whole` workgroups have a tile of W each; the others share theirs, by the rows, with splits - 1 more
+  const int shared = (int)blockIdx.x - whole;
+  const int tile = shared < 0 ? blockIdx.x : whole + shared / splits;
+  const int part = shared < 0 ? 0 : shared % splits, parts = shared < 0 ? 1 : splits;
   // the stream's buffers; after it a tile of each wave
   static_assert(kBuffers >= kWaves, "the stream's buffers hold the waves' own tiles");
   __shared__ Tile<D> tiles[kBuffers];
   __shared__ float2 stats[kBuffers][kWaves][kTile];   // of a tile's rows, a copy for each wave
-  __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients where a group has many entries
+  __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients of the teacher's entries
+  __shared__ int range[2][kWaves];
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, t = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int64_t x0 = (int64_t)blockIdx.x * kHold + wave * 64;
-  const int nt = TileStream<D>::count(rows);
+  const int64_t x0 = (int64_t)tile * kHold + wave * 64;
+  const int all = TileStream<D>::count(rows);
+  const int t0 = (int)((int64_t)all * part / parts), nt = (int)((int64_t)all * (part + 1) / parts);
   const TileStream<D> rho_tiles(rho, rows, r);
   auto stream = [&](int tile, int to) {
     stream_to_lds4(row_stats + (size_t)tile * kTile, 4 * lane, lds_address(stats[to][wave]));
@@ -680,13 +731,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   hold_load<D>(xf, W, x0, V, r);
   f32x16 o[2][D / 32] = {};
   constexpr int kLoads = Tile<D>::kLoads + 1;
-  for (int i = 0; i < 3; ++i) stream(min(i, nt - 1), i);
+  for (int i = 0; i < 3; ++i) stream(min(t0 + i, nt - 1), i);
   stream_wait<2 * kLoads>();
   __syncthreads();
   bf16x8 a[kAhead], p[2][2] = {};   // as in k_head_rho
   pieces_first(a, tiles[0]);
   int at = 0, before = 0;
-  for (int k = 0; k < nt; ++k) {
+  for (int k = t0; k < nt; ++k) {
     const int next = next_buffer(at), free = next_buffer(next_buffer(next));
     const float2* st = stats[at][wave];
     f32x16 s[2];
@@ -716,49 +767,112 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   stream_wait<0>();
   __syncthreads();
   // The teacher's entries of this wave's 64 rows of W, in order of the row.  Few of them: 32 entries a tile, each with
-  // its own row of rho and one coefficient.  Many (frequent tokens): by tiles of 32 successive rows, with all of a
-  // tile's coefficients, so that no group takes longer than the rows did.
-  const uint32_t b0 = begin[blockIdx.x * kWaves + wave], b1 = begin[blockIdx.x * kWaves + wave + 1];
-  const Tile<D>& own = tiles[wave];
+  // its own row of rho and one coefficient.  Where any wave has many (frequent tokens): the tiles of rho once more for
+  // all four, with every coefficient that a tile's rows have, so that no list takes much longer than the rows did.
+  const uint32_t l0 = begin[tile * kWaves + wave], ln = begin[tile * kWaves + wave + 1] - l0;
+  const uint32_t b1 = l0 + (uint32_t)((uint64_t)ln * (part + 1) / parts);
+  uint32_t b = l0 + (uint32_t)((uint64_t)ln * part / parts);
   float* q = wide[wave];
-  const bool few = (b1 - b0 + kTile - 1) / kTile <= (uint32_t)nt;
-  for (uint32_t b = b0; b < b1;) {
-    uint2 en = list[min(b + lane, b1 - 1)];
-    const uint32_t tile = __builtin_amdgcn_readfirstlane(en.x & 0xffffffu) / kTile;
-    const uint32_t mine = few ? en.x & 0xffffffu : (uint32_t)min((int64_t)tile * kTile + n, rows - 1);   // lane m: tile row m's
-    lds_done();
-    wave_tile_stream(own, rho, mine, r);
 #pragma unroll
-    for (int i = 0; i < kTile * kHeadGroup / 256; ++i)
-      *reinterpret_cast<float4*>(q + (i * 64 + lane) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (;;) {   // many: the entries of the tile's rows are a run of the list
-      const bool in = b + lane < b1 && (few ? lane < kTile : (en.x & 0xffffffu) / kTile == tile);
-      // (one wave's LDS additions happen in its own order: repeated ids always add up the same way)
-      if (in) unsafeAtomicAdd(q + (few ? lane : en.x % kTile) * kHeadGroup + (en.x >> 24), __uint_as_float(en.y));
-      const int found = __popcll(__builtin_amdgcn_ballot_w64(in));
-      b += found;
-      if (found < 64 || b >= b1) break;
-      en = list[min(b + lane, b1 - 1)];
+  for (int i = 0; i < kTile * kHeadGroup / 256; ++i) *reinterpret_cast<float4*>(q + (i * 64 + lane) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+  // (a tile of entries takes about two and a half times as long as one of rows)
+  const bool many = __syncthreads_or((b1 - b + kTile - 1) / kTile > (uint32_t)(nt - t0) * 2 / 5);
+  const uint32_t end = max(b1, 1u) - 1;
+  uint2 en[4];   // many: the next 256 entries; few: 32
+#pragma unroll
+  for (int u = 0; u < 4; ++u) en[u] = list[min(b + (many ? u * 64 + lane : n), end)];
+  int k = 0, last = 0;
+  at = 0;
+  if (many) {   // (lists are shared by position, rows by tile: a part's entries may begin before and end after its rows)
+    if (lane == 0) {
+      range[0][wave] = b < b1 ? (int)((list[b].x & 0xffffffu) / kTile) : all;
+      range[1][wave] = b < b1 ? (int)((list[b1 - 1].x & 0xffffffu) / kTile) + 1 : 0;
     }
-    stream_wait<0>();
-    lds_done();
-#pragma unroll 1
-    for (int rest = 0; rest < 2; ++rest) {
-      coefficients(p, q, rest);
-      product_o<D>(o, own, p, [](int) {});
-    }
+    __syncthreads();
+    k = __builtin_amdgcn_readfirstlane(min(min(range[0][0], range[0][1]), min(range[0][2], range[0][3])));
+    last = __builtin_amdgcn_readfirstlane(max(max(range[1][0], range[1][1]), max(range[1][2], range[1][3])));
+    for (int i = 0; i < 3; ++i) rho_tiles.start(tiles[i], min(k + i, all - 1));
   }
+  while (many ? k < last : b < b1) {
+    const uint32_t from = b;
+    int first = 0;
+    if (many) {
+      stream_wait<2 * Tile<D>::kLoads>();   // (the loads of entries only make it wait for more)
+      __syncthreads();
+      rho_tiles.start(tiles[next_buffer(next_buffer(next_buffer(at)))], min(k + 3, all - 1));
+      first = (int)TileStream<D>::first(k, rows);
+      for (;;) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t row = en[u].x & 0xffffffu;
+          const bool in = b + u * 64 + lane < b1 && (int)(row / kTile) == k;
+          // (one wave's LDS additions happen in its own order: repeated ids always add up the same way)
+          if (in) unsafeAtomicAdd(q + (row - first) * kHeadGroup + (en[u].x >> 24), __uint_as_float(en[u].y));
+          found += __popcll(__builtin_amdgcn_ballot_w64(in));
+        }
+        b += found;
+        if (found < 256 || b >= b1) break;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) en[u] = list[min(b + u * 64 + lane, end)];
+      }
+      ++k;
+    } else {
+      lds_done();
+      wave_tile_stream(tiles[wave], rho, en[0].x & 0xffffffu, r);
+      if (h == 0 && b + n < b1) q[n * kHeadGroup + (en[0].x >> 24)] = __uint_as_float(en[0].y);
+      b = min(b + kTile, b1);
+      en[1] = en[0];
+      en[0] = list[min(b + n, end)];   // (the next tile's)
+      stream_wait<0>();
+    }
+    if (b > from) {
+      lds_done();
+      coefficient_products<D>(o, tiles[many ? at : wave], q);
+      if (many) {
+        for (uint32_t i = from + lane; i < b; i += 64) {
+          const uint32_t x = list[i].x;
+          q[((x & 0xffffffu) - first) * kHeadGroup + (x >> 24)] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) en[u] = list[min(b + u * 64 + lane, end)];
+      } else if (h == 0) {
+        q[n * kHeadGroup + (en[1].x >> 24)] = 0.f;
+      }
+    }
+    at = next_buffer(at);
+  }
+  stream_wait<0>();
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int64_t v = x0 + 32 * x + 8 * (i >> 2) + 4 * h + (i & 3);
-      if (v >= V) continue;
-      bf16_t* out = d_w + (size_t)v * r;
+      const int m = 32 * x + 8 * (i >> 2) + 4 * h + (i & 3);
+      if (x0 + m >= V) continue;
+      if (shared < 0) {
+        bf16_t* out = d_w + (size_t)(x0 + m) * r;
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-        if (32 * dt + n < r) out[32 * dt + n] = __builtin_bit_cast(bf16_t, (__bf16)o[x][dt][i]);
+        for (int dt = 0; dt < D / 32; ++dt)
+          if (32 * dt + n < r) out[32 * dt + n] = __builtin_bit_cast(bf16_t, (__bf16)o[x][dt][i]);
+      } else {
+        float* out = part_w + ((size_t)shared * kHold + wave * 64 + m) * r;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          if (32 * dt + n < r) out[32 * dt + n] = o[x][dt][i];
+      }
     }
+}
+
+// the parts of the shared tiles, eight elements a thread
+__global__ __launch_bounds__(kThreads) void k_head_join(const float* __restrict__ part_w, int splits, int64_t first,
+                                                        int V, int r, bf16_t* __restrict__ d_w) {
+  const int64_t per = (int64_t)kHold * r, e = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8;
+  const int64_t tile = e / per, in = e % per;
+  if (first + tile * kHold + in / r >= V) return;
+  const float* from = part_w + tile * splits * per + in;
+  f32x8 sum = *reinterpret_cast<const f32x8*>(from);
+  for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x8*>(from + s * per);
+  *reinterpret_cast<bf16x8*>(d_w + first * r + e) = __builtin_convertvector(sum, bf16x8);
 }
 
 __global__ __launch_bounds__(kThreads) void k_zero(uint4* __restrict__ p, int64_t n) {
@@ -766,11 +880,13 @@ __global__ __launch_bounds__(kThreads) void k_zero(uint4* __restrict__ p, int64_
   if (i < n) p[i] = make_uint4(0, 0, 0, 0);
 }
 
-int head_splits(int64_t rows, int V) {
-  // about one workgroup per CU (a wave holds a SIMD's registers), each split at least 8 tiles
+// Workgroups at a time: one per CU, a wave of rank 256 or 128 with gradients holding its SIMD's registers, else two
+constexpr int kSlots = 256;
+int head_splits(int64_t rows, int V, bool grads) {
+  // of the vocabulary, where rho is held: a slot each; every split at least 8 tiles
   const int64_t blocks = (rows + kHold - 1) / kHold;
-  const int64_t cap = std::max<int64_t>(1, V / (8 * kTile));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 / std::max<int64_t>(1, blocks), cap), 256));
+  const int64_t cap = std::max<int64_t>(1, V / (8 * kTile)), slots = grads ? kSlots : 2 * kSlots;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / std::max<int64_t>(1, blocks), cap), kHeadMostSplits));
 }
 
 template <int D>
@@ -810,8 +926,13 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_sort_place<<<(unsigned)l.chunks, 64, key_bytes, st>>>(a.teacher, n, a.V, l.keys, l.chunk, counts, begin, o.coef, list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_head_w<D><<<(unsigned)l.tiles, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher.c, o.row, begin, list,
-                                                      (bf16_t*)a.d_w);
+  float* part_w = (float*)(a.ws + l.off_o);   // (the splits' sums are joined by now)
+  k_head_w<D><<<(unsigned)(l.whole + (l.tiles - l.whole) * l.row_splits), kThreads, 0, st>>>(
+      rho, W, a.rows, a.V, a.r, a.teacher.c, o.row, begin, list, l.whole, l.row_splits, (bf16_t*)a.d_w, part_w);
+  if ((e = hipGetLastError()) != hipSuccess || l.whole == l.tiles) return e;
+  const int64_t elems = (int64_t)(l.tiles - l.whole) * kHold * a.r;
+  k_head_join<<<(unsigned)((elems / 8 + kThreads - 1) / kThreads), kThreads, 0, st>>>(part_w, l.row_splits, (int64_t)l.whole * kHold,
+                                                                                  a.V, a.r, (bf16_t*)a.d_w);
   return hipGetLastError();
 }
 
@@ -820,9 +941,13 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
 HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads) {
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   HeadLayout l = {};
-  l.splits = head_splits(rows, V);
+  l.splits = head_splits(rows, V, grads);
   l.tiles = (V + kHold - 1) / kHold;
   l.keys = l.tiles * (kHold / kHeadGroup);   // every wave's, also past V
+  // the tiles that the last round of workgroups has too few of share a slot's rows: parts of at least 8 tiles of rows
+  const int left = l.tiles % kSlots;
+  l.row_splits = left ? (int)std::max<int64_t>(1, std::min<int64_t>(kSlots / left, rows / (8 * kTile))) : 1;
+  l.whole = l.row_splits > 1 ? l.tiles - left : l.tiles;
   const int64_t n = rows * k;
   // chunks of at least 512 entries, at most 1,024 of them
   l.chunk = (int)std::max<int64_t>(512, ((n + 1023) / 1024 + 63) / 64 * 64);
@@ -830,7 +955,7 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
   size_t at = up((size_t)l.splits * rows * sizeof(float2));
   if (grads) {
     l.off_o = at;
-    at += up((size_t)l.splits * rows * r * sizeof(float));
+    at += up(std::max((size_t)l.splits * rows, (size_t)(l.tiles - l.whole) * l.row_splits * kHold) * r * sizeof(float));
     l.off_row = at;
     at += up((size_t)(rows + kTile) * sizeof(float2));
     l.off_coef = at;

@@ -93,6 +93,14 @@ def test_matches_float64(rows, V, r, K, renorm):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,V,r", [(2100, 600, 256), (1500, 513, 64), (4097, 2000, 128)])
+def test_tiles_of_w_shared_by_workgroups(rows, V, r):
+    """Fewer tiles of W than CUs and many rows: the rows are split and the parts joined."""
+    rho, w, ids, y, weight = _make(rows, V, r, 24, rows, ragged=True)
+    _check(rho, w, ids, y, weight, 1.0, True, B.head_distill(rho, w, ids, y, grad_loss=weight, want_grads=True))
+
+
+@pytest.mark.gpu
 def test_the_main_vocabulary():
     rho, w, ids, y, weight = _make(40, 151936, 256, 64, 5)
     _check(rho, w, ids, y, weight, 1.0, True, B.head_distill(rho, w, ids, y, grad_loss=weight, want_grads=True))

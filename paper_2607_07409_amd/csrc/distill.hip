@@ -21,12 +21,12 @@ struct LossOut {
 // the loss of a row from its sums, by the whole workgroup
 template <typename T>
 __device__ __forceinline__ void finish_row(const T* row, int V, int64_t r, const RowSum& a, const TeacherArgs& te,
-                                           TeacherShared& sh, const LossOut& o) {
+                                           TeacherShared<kThreads>& sh, const LossOut& o) {
   float mass;
-  const TeacherEntry e = teacher_entry(te, r, V, sh, &mass);
+  const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, r, V), sh, &mass);
   const float l2 = a.s > 0.f ? fast_log2(a.s) : 0.f;
   const float x = e.id >= 0 ? to_f32(row[e.id]) : -INFINITY;
-  const float loss = block_sum(teacher_term(e, above_ref(x, te.c, a.R) - l2), sh.red);
+  const float loss = block_sum<kThreads>(teacher_term(e, above_ref(x, te.c, a.R) - l2), sh.red);
   if (threadIdx.x == 0) {
     if (o.loss) o.loss[r] = loss;
     if (o.lse) o.lse[r] = row_lse(a);
@@ -38,8 +38,8 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__ L, int V, int64_t stride, TeacherArgs te,
                                                            float2* __restrict__ part_sums, LossOut o) {
   constexpr int N = Chunk<T>::N;
-  __shared__ RowShared shr;
-  __shared__ TeacherShared sht;
+  __shared__ RowShared<> shr;
+  __shared__ TeacherShared<kThreads> sht;
   const int part = blockIdx.y, parts = gridDim.y;
   const int64_t r = blockIdx.x;
   const T* row = L + (size_t)r * stride;
@@ -59,8 +59,8 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void k_distill_finish(const T* __restrict__ L, int V, int64_t stride,
                                                              TeacherArgs te, int parts,
                                                              const float2* __restrict__ part_sums, LossOut o) {
-  __shared__ RowShared shr;
-  __shared__ TeacherShared sht;
+  __shared__ RowShared<> shr;
+  __shared__ TeacherShared<kThreads> sht;
   const int64_t r = blockIdx.x;
   RowSum a = row_empty();
   if ((int)threadIdx.x < parts) {   // parts <= 256
@@ -93,13 +93,96 @@ template <> struct Store<bf16_t> {
   __device__ __forceinline__ static void one(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
 };
 
+// Loss and gradient with the row on chip: a workgroup of NT threads reads its row once, NCH 16-byte pieces a thread,
+// into registers, and writes the gradient from there.  All of a row's loads are in flight together.
+template <typename T, int NT, int NCH>
+__global__ __launch_bounds__(NT) void k_distill_row(const T* L, int V, int64_t stride, TeacherArgs te,
+                                                    const float* __restrict__ weight, LossOut o, T* G, int64_t gstride) {
+  constexpr int N = Chunk<T>::N;
+  __shared__ RowShared<NT> shr;
+  __shared__ TeacherShared<NT> sht;
+  __shared__ int ids[256];
+  __shared__ float qs[256];
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const T* row = L + (size_t)r * stride;
+  T* out = G + (size_t)r * gstride;
+  const RowRange g = row_range(row, V, 0, 1);
+  // (one address for the row and 32-bit offsets: the registers are needed for the row itself)
+  const char* from = reinterpret_cast<const char*>(row + g.h0);
+  char* to = reinterpret_cast<char*>(out + g.h0);
+  uint4 raw[NCH];
+  if (g.c1 > 0) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) raw[i] = stream_load16(from + (uint32_t)min(t + i * NT, g.c1 - 1) * 16u);
+  }
+  const TeacherRaw tr = teacher_raw(te, r, V);
+  const float xk = tr.id >= 0 ? to_f32(row[tr.id]) : -INFINITY;   // read before anything is written: G may be L
+  RowSum a = row_empty();
+  float edge[2] = {0.f, 0.f};   // this thread's entry before the first piece, and behind the last
+  const bool has[2] = {t < g.h0, t < V - g.tail0};
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (has[e]) {
+      edge[e] = to_f32(row[e == 0 ? t : g.tail0 + t]);
+      row_fold<1, false>(a, &edge[e], edge[e], te.c);
+    }
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+    if (t + i * NT < g.c1) {
+      float x[N];
+      Chunk<T>::widen(raw[i], x);
+      row_fold<N, false>(a, x, max_of<N>(x), te.c);
+    }
+  a = row_block_merge<false>(a, shr);
+  float mass;
+  const TeacherEntry e = teacher_entry<NT>(te, tr, sht, &mass);
+  if (t < 256) {
+    ids[t] = e.id;
+    qs[t] = e.q;
+  }
+  const float l2 = a.s > 0.f ? fast_log2(a.s) : 0.f;
+  const float loss = block_sum<NT>(teacher_term(e, above_ref(xk, te.c, a.R) - l2), sht.red);   // (its barriers cover ids, qs)
+  if (t == 0) {
+    if (o.loss) o.loss[r] = loss;
+    if (o.lse) o.lse[r] = row_lse(a);
+  }
+  const float w = (weight ? weight[r] : 1.f) * te.inv_temp, f = a.s > 0.f ? w * mass / a.s : 0.f;
+  auto dense = [&](float x) { return f * fast_exp2(fminf(above_ref(x, te.c, a.R), 126.f)); };
+  bool mine = e.id >= 0;
+  float entry = 0.f;
+  if (mine) {
+    float q = 0.f;
+    for (int j = 0; j < te.k; ++j) {
+      const bool same = ids[j] == e.id;
+      q += same ? qs[j] : 0.f;
+      mine = mine && !(same && j < t);
+    }
+    entry = dense(xk) - w * q;
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (has[e]) Store<T>::one(out + (e == 0 ? t : g.tail0 + t), dense(edge[e]));
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+    if (t + i * NT < g.c1) {
+      float x[N], d[N];
+      Chunk<T>::widen(raw[i], x);
+#pragma unroll
+      for (int k = 0; k < N; ++k) d[k] = dense(x[k]);
+      Store<T>::chunk(reinterpret_cast<T*>(to + (uint32_t)(t + i * NT) * 16u), d);
+    }
+  __syncthreads();   // the row is written before its teacher entries are
+  if (mine) Store<T>::one(out + e.id, entry);
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, int64_t stride, TeacherArgs te,
                                                            const float* __restrict__ lse,
                                                            const float2* __restrict__ row_stats,
                                                            const float* __restrict__ weight, T* G, int64_t gstride) {
   constexpr int N = Chunk<T>::N;
-  __shared__ TeacherShared sht;
+  __shared__ TeacherShared<kThreads> sht;
   __shared__ int ids[kThreads];
   __shared__ float qs[kThreads];
   const int part = blockIdx.y, parts = gridDim.y, t = threadIdx.x;
@@ -108,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, in
   T* out = G + (size_t)r * gstride;
   const RowRange g = row_range(row, V, part, parts);
   float mass;
-  const TeacherEntry e = teacher_entry(te, r, V, sht, &mass);
+  const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, r, V), sht, &mass);
   ids[t] = e.id;
   qs[t] = e.q;
   __syncthreads();
@@ -173,8 +256,29 @@ hipError_t launch_grad_t(const DistillArgs& a, const float2* row_stats, hipStrea
   return hipGetLastError();
 }
 
+// A row whose pieces fit a workgroup's registers is read once
+template <typename T, int NT, int NCH>
+hipError_t launch_row_t(const DistillArgs& a, hipStream_t st) {
+  const LossOut o = {a.out_loss, a.out_lse, nullptr};
+  k_distill_row<T, NT, NCH><<<(unsigned)a.rows, NT, 0, st>>>((const T*)a.logits, a.V, a.stride, a.teacher, a.weight, o,
+                                                             (T*)a.grad, a.grad_stride);
+  return hipGetLastError();
+}
+template <typename T>
+bool row_fits(int32_t V) { return V <= 1024 * 20 * Chunk<T>::N; }
+template <typename T>
+hipError_t launch_row(const DistillArgs& a, hipStream_t st) {
+  const int64_t pieces = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
+  if (a.rows >= 512 && pieces <= 256 * 20) return launch_row_t<T, 256, 20>(a, st);
+  if (a.rows >= 512 && pieces <= 512 * 20) return launch_row_t<T, 512, 20>(a, st);
+  return pieces <= 1024 * 5    ? launch_row_t<T, 1024, 5>(a, st)
+         : pieces <= 1024 * 10 ? launch_row_t<T, 1024, 10>(a, st)
+                               : launch_row_t<T, 1024, 20>(a, st);
+}
+
 template <typename T>
 hipError_t launch_loss_t(const DistillArgs& a, hipStream_t st) {
+  if (a.grad && row_fits<T>(a.V)) return launch_row<T>(a, st);
   const int parts = row_parts(a.rows, a.V, (int)sizeof(T));
   float2* rows = (float2*)a.ws;
   float2* sums = rows + a.rows;

@@ -445,8 +445,8 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
                                                           const float* __restrict__ weight, int splits,
                                                           const float2* __restrict__ part_sum,
                                                           const float* __restrict__ part_o, HeadOut o) {
-  __shared__ RowShared shr;
-  __shared__ TeacherShared sht;
+  __shared__ RowShared<> shr;
+  __shared__ TeacherShared<kThreads> sht;
   __shared__ float q[256], log_q[256], scale[kHeadMostSplits];
   __shared__ int id[256];
   __shared__ float4 acc[kWaves][64];
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t row = blockIdx.x;
   float mass;
-  const TeacherEntry e = teacher_entry(te, row, V, sht, &mass);
+  const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, row, V), sht, &mass);
   q[t] = e.q;
   log_q[t] = e.log_q;
   id[t] = e.id;

@@ -73,36 +73,37 @@ __device__ __forceinline__ RowSum row_merge(RowSum a, RowSum b) {
   return {R, a.s + b.s, ENT ? a.t + b.t : 0.f};
 }
 
-// over the 64 lanes of a wave, the same in every lane: the largest reference first, then one rescale and a sum
-template <bool ENT>
+// over groups of W lanes, the same in every lane: the largest reference first, then one rescale and a sum
+template <bool ENT, int W = 64>
 __device__ __forceinline__ RowSum row_wave_merge(RowSum a) {
   float R = a.R;
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) R = fmaxf(R, __shfl_xor(R, k));
+  for (int k = W / 2; k >= 1; k >>= 1) R = fmaxf(R, __shfl_xor(R, k));
   row_rescale<ENT>(a, R);
-  a.s = wave_sum(a.s);
-  if (ENT) a.t = wave_sum(a.t);
+#pragma unroll
+  for (int k = W / 2; k >= 1; k >>= 1) {
+    a.s += __shfl_xor(a.s, k);
+    if (ENT) a.t += __shfl_xor(a.t, k);
+  }
   return a;
 }
 
-// over a workgroup of 256 threads, in a fixed order; every thread gets the total
+// over a workgroup of NT threads, in a fixed order; every thread gets the total
+template <int NT = kRowThreads>
 struct RowShared {
-  float R[kRowThreads / 64], s[kRowThreads / 64], t[kRowThreads / 64];
+  float R[NT / 64], s[NT / 64], t[NT / 64];
 };
-template <bool ENT>
-__device__ __forceinline__ RowSum row_block_merge(RowSum a, RowShared& sh) {
+template <bool ENT, int NT>
+__device__ __forceinline__ RowSum row_block_merge(RowSum a, RowShared<NT>& sh) {
   a = row_wave_merge<ENT>(a);
-  const int wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6, from = threadIdx.x % (NT / 64);
   if ((threadIdx.x & 63) == 0) {
     sh.R[wave] = a.R;
     sh.s[wave] = a.s;
     if (ENT) sh.t[wave] = a.t;
   }
   __syncthreads();
-  RowSum b = {sh.R[0], sh.s[0], ENT ? sh.t[0] : 0.f};
-#pragma unroll
-  for (int w = 1; w < kRowThreads / 64; ++w) b = row_merge<ENT>(b, RowSum{sh.R[w], sh.s[w], ENT ? sh.t[w] : 0.f});
-  return b;
+  return row_wave_merge<ENT, NT / 64>(RowSum{sh.R[from], sh.s[from], ENT ? sh.t[from] : 0.f});
 }
 
 // natural log-sum-exp; -inf for a row without an entry above -inf

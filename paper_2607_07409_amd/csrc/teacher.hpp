@@ -10,51 +10,62 @@ struct TeacherEntry {
   float q, log_q;    // log q natural; q = 0 for an absent entry
 };
 
+template <int NT>
 struct TeacherShared {
-  float red[kRowThreads / 64];
+  float red[NT / 64];
 };
 
-// sum (or maximum) over the workgroup, in a fixed order, in every thread
-__device__ __forceinline__ float block_sum(float v, float* red) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-__device__ __forceinline__ float block_max(float v, float* red) {
+// sum (or maximum) over a workgroup of NT threads, in a fixed order, in every thread
+template <int NT, typename Op>
+__device__ __forceinline__ float block_reduce(float v, float* red, Op op) {
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) v = fmaxf(v, __shfl_xor(v, k));
+  for (int k = 32; k >= 1; k >>= 1) v = op(v, __shfl_xor(v, k));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  v = red[threadIdx.x % (NT / 64)];
+#pragma unroll
+  for (int k = NT / 128; k >= 1; k >>= 1) v = op(v, __shfl_xor(v, k));
+  return v;
+}
+template <int NT>
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  return block_reduce<NT>(v, red, [](float a, float b) { return a + b; });
+}
+template <int NT>
+__device__ __forceinline__ float block_max(float v, float* red) {
+  return block_reduce<NT>(v, red, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// This thread's entry of row r, and the row's mass sum_k q_k (1 or 0 where normalised).
-__device__ __forceinline__ TeacherEntry teacher_entry(const TeacherArgs& te, int64_t r, int V, TeacherShared& sh,
-                                                      float* mass) {
-  const int t = threadIdx.x;
-  TeacherEntry e = {-1, 0.f, -INFINITY};
-  float y = -INFINITY;
-  if (t < te.k) {
-    const size_t at = (size_t)r * te.k + t;
+// This thread's entry of row r as it is stored: id -1 and -inf for an absent one.
+struct TeacherRaw {
+  int id;
+  float y;
+};
+__device__ __forceinline__ TeacherRaw teacher_raw(const TeacherArgs& te, int64_t r, int V) {
+  TeacherRaw e = {-1, -INFINITY};
+  if ((int)threadIdx.x < te.k) {
+    const size_t at = (size_t)r * te.k + threadIdx.x;
     e.id = te.ids[at];
-    y = te.values[at];
-    if (e.id < 0 || e.id >= V || !(y > -INFINITY)) {
-      e.id = -1;
-      y = -INFINITY;
-    }
+    e.y = te.values[at];
+    if (e.id < 0 || e.id >= V || !(e.y > -INFINITY)) e = TeacherRaw{-1, -INFINITY};
   }
+  return e;
+}
+// This thread's entry, and the row's mass sum_k q_k (1 or 0 where normalised).
+template <int NT>
+__device__ __forceinline__ TeacherEntry teacher_entry(const TeacherArgs& te, TeacherRaw raw, TeacherShared<NT>& sh,
+                                                      float* mass) {
+  TeacherEntry e = {raw.id, 0.f, -INFINITY};
   if (te.logprobs) {
-    e.q = fast_exp2(y * kLog2e);
-    e.log_q = y;
-    *mass = block_sum(e.q, sh.red);
+    e.q = fast_exp2(raw.y * kLog2e);
+    e.log_q = raw.y;
+    *mass = block_sum<NT>(e.q, sh.red);
   } else {
-    const float top = block_max(y, sh.red);
-    const float d = e.id < 0 ? -INFINITY : (y - top) * te.c;   // (the largest finite values differ by a finite amount)
+    const float top = block_max<NT>(raw.y, sh.red);
+    const float d = e.id < 0 ? -INFINITY : (raw.y - top) * te.c;   // (the largest finite values differ by a finite amount)
     const float w = fast_exp2(d);
-    const float sum = block_sum(w, sh.red);
+    const float sum = block_sum<NT>(w, sh.red);
     e.q = sum > 0.f ? w / sum : 0.f;
     e.log_q = e.id < 0 ? -INFINITY : (d - fast_log2(sum)) * kLn2;
     *mass = sum > 0.f ? 1.f : 0.f;

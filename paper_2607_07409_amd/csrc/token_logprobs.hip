@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
                                                             int segs, float4* __restrict__ part_sums,
                                                             u64* __restrict__ part_keys) {
   constexpr int N = Chunk<T>::N, NT = kThreads;
-  __shared__ RowShared shr;
+  __shared__ RowShared<> shr;
   __shared__ Select sh;
   __shared__ u64 blocks[TOP ? kMostSegs * NT : 1];
   __shared__ u64 list[TOP ? kCand : 1];
@@ -255,7 +255,7 @@ template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict__ L, int V, int64_t stride, RowOut o,
                                                              int parts, const float4* __restrict__ part_sums,
                                                              const u64* __restrict__ part_keys) {
-  __shared__ RowShared shr;
+  __shared__ RowShared<> shr;
   __shared__ Select sh;
   __shared__ u64 list[TOP ? kCand : 1];
   const int t = threadIdx.x;

@@ -93,6 +93,32 @@ template <> struct Store<bf16_t> {
   __device__ __forceinline__ static void one(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
 };
 
+// The dense part of a gradient, f 2^(y - R), of n entries.  R is the same in every lane of the workgroup, so the choice is
+// a scalar branch; a clamped R holds no difference of the size of a logarithm, so there a probability is at most 1.
+struct Dense {
+  float c, R, f;
+  bool plain;
+  __device__ __forceinline__ Dense(float c, float R_, float f) : c(c), f(f) {
+    R = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(R_)));
+    plain = fabsf(R) < kPlainRef;
+  }
+  template <int n>
+  __device__ __forceinline__ void operator()(const float* x, float* d) const {
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) d[i] = f * fast_exp2(__builtin_fmaf(x[i], c, -R));
+    } else {
+#pragma unroll
+      for (int i = 0; i < n; ++i) d[i] = f * fast_exp2(fminf(above_ref(x[i], c, R), 0.f));
+    }
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    float d;
+    operator()<1>(&x, &d);
+    return d;
+  }
+};
+
 // Loss and gradient with the row on chip: a workgroup of NT threads reads its row once, NCH 16-byte pieces a thread,
 // into registers, and writes the gradient from there.  All of a row's loads are in flight together.
 template <typename T, int NT, int NCH>
@@ -148,7 +174,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(const T* L, int V, int64_t s
     if (o.lse) o.lse[r] = row_lse(a);
   }
   const float w = (weight ? weight[r] : 1.f) * te.inv_temp, f = a.s > 0.f ? w * mass / a.s : 0.f;
-  auto dense = [&](float x) { return f * fast_exp2(fminf(above_ref(x, te.c, a.R), 126.f)); };
+  const Dense dense(te.c, a.R, f);
   bool mine = e.id >= 0;
   float entry = 0.f;
   if (mine) {
@@ -168,14 +194,16 @@ __global__ __launch_bounds__(NT) void k_distill_row(const T* L, int V, int64_t s
     if (t + i * NT < g.c1) {
       float x[N], d[N];
       Chunk<T>::widen(raw[i], x);
-#pragma unroll
-      for (int k = 0; k < N; ++k) d[k] = dense(x[k]);
+      dense.template operator()<N>(x, d);
       Store<T>::chunk(reinterpret_cast<T*>(to + (uint32_t)(t + i * NT) * 16u), d);
     }
   __syncthreads();   // the row is written before its teacher entries are
   if (mine) Store<T>::one(out + e.id, entry);
 }
 
+// The gradient of a part of a row, at most kGradPieces 16-byte pieces a thread, whose loads are all on their way before
+// the teacher's entries are looked at.  The row's sums come from the loss pass, or from its log-sum-exp.
+constexpr int kGradPieces = 10;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, int64_t stride, TeacherArgs te,
                                                            const float* __restrict__ lse,
@@ -190,11 +218,22 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, in
   const T* row = L + (size_t)r * stride;
   T* out = G + (size_t)r * gstride;
   const RowRange g = row_range(row, V, part, parts);
-  float mass;
-  const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, r, V), sht, &mass);
-  ids[t] = e.id;
-  qs[t] = e.q;
-  __syncthreads();
+  uint4 raw[kGradPieces];
+  if (g.c1 > g.c0) {
+#pragma unroll
+    for (int i = 0; i < kGradPieces; ++i)
+      raw[i] = stream_load16(row + g.h0 + (size_t)min(g.c0 + t + i * kThreads, g.c1 - 1) * N);
+  }
+  const TeacherRaw tr = teacher_raw(te, r, V);
+  // my entry, where its id lies in this part's range: read before anything is written, G may be L
+  const int lo = part == 0 ? 0 : g.h0 + g.c0 * N, hi = part == parts - 1 ? V : g.h0 + g.c1 * N;
+  bool mine = tr.id >= lo && tr.id < hi;
+  const float xk = mine ? to_f32(row[tr.id]) : 0.f;
+  float edge[2] = {0.f, 0.f};   // this thread's entry before the row's first piece, and behind its last
+  const bool has[2] = {part == 0 && t < g.h0, part == parts - 1 && t < V - g.tail0};
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (has[e]) edge[e] = to_f32(row[e == 0 ? t : g.tail0 + t]);
   // softmax(s / T)_v = 2^(y - R) f
   float R, f;
   if (row_stats) {
@@ -209,43 +248,43 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, in
         : fabsf(R) < kPlainRef ? fast_exp2(-(__builtin_fmaf(l, kLog2e, -R) + l * kLog2eLow)) : 1.f;
   }
   const float w = (weight ? weight[r] : 1.f) * te.inv_temp;
-  const float a = w * mass * f;
-  // (a clamped R holds no difference of the size of a logarithm: a probability is then at most 1)
-  const float most = fabsf(R) < kPlainRef ? 126.f : 0.f;
-  auto dense = [&](float x) { return a * fast_exp2(fminf(above_ref(x, te.c, R), most)); };
-
-  // my entry, if its id lies in this part's range and no earlier entry has the same id
-  const int lo = part == 0 ? 0 : g.h0 + g.c0 * N, hi = part == parts - 1 ? V : g.h0 + g.c1 * N;
-  bool mine = e.id >= lo && e.id < hi;
+  float mass;
+  const TeacherEntry e = teacher_entry<kThreads>(te, tr, sht, &mass);
+  ids[t] = e.id;
+  qs[t] = e.q;
+  __syncthreads();   // (also: every entry of the teacher's has been read)
+  const Dense dense(te.c, R, w * mass * f);
   float entry = 0.f;
-  if (mine) {
+  if (mine) {   // several entries of one id are the first one's
     float q = 0.f;
     for (int j = 0; j < te.k; ++j) {
       const bool same = ids[j] == e.id;
       q += same ? qs[j] : 0.f;
       mine = mine && !(same && j < t);
     }
-    entry = dense(to_f32(row[e.id])) - w * q;   // read before anything is written: G may be L
+    entry = dense(xk) - w * q;
   }
-  __syncthreads();
-  row_edges(g, V, part, parts, [&](int v) { Store<T>::one(out + v, dense(to_f32(row[v]))); });
-  row_chunks(
-      row, g,
-      [&](int c, const float* x, float) {
-        float d[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) d[i] = dense(x[i]);
-        Store<T>::chunk(out + g.h0 + (size_t)c * N, d);
-      },
-      [](int) {});
-  __syncthreads();   // the pass over the range is written before its teacher entries are
+  for (int e = 0; e < 2; ++e)
+    if (has[e]) Store<T>::one(out + (e == 0 ? t : g.tail0 + t), dense(edge[e]));
+#pragma unroll
+  for (int i = 0; i < kGradPieces; ++i) {
+    const int c = g.c0 + t + i * kThreads;
+    if (c < g.c1) {
+      float x[N], d[N];
+      Chunk<T>::widen(raw[i], x);
+      dense.template operator()<N>(x, d);
+      Store<T>::chunk(out + g.h0 + (size_t)c * N, d);
+    }
+  }
+  __syncthreads();   // the part is written before its teacher entries are
   if (mine) Store<T>::one(out + e.id, entry);
 }
 
-// workgroups per row of the gradient pass: ranges of about 32 KiB, more where rows are few
+// workgroups per row of the gradient pass: as many as its pieces need, more where rows are few
 int grad_parts(int64_t rows, int32_t V, int elem_bytes) {
-  const int64_t few = row_parts(rows, V, elem_bytes), fit = ((int64_t)V * elem_bytes + 32767) / 32768;
-  return (int)std::max<int64_t>(1, std::max(few, fit));
+  const int64_t few = row_parts(rows, V, elem_bytes), per = (int64_t)kThreads * kGradPieces * (16 / elem_bytes);
+  return (int)std::max<int64_t>(1, std::max<int64_t>(few, (V + per - 1) / per));
 }
 
 template <typename T>

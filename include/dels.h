@@ -382,7 +382,7 @@ dls_status dls_unigram_log_prior(const int32_t *tokens, int64_t n, int32_t V, fl
  *   logits           [rows, V] of `dtype`, row_stride >= V elements apart, the entries of a row
  *                    contiguous; any alignment of the element type
  *   tokens           [rows] int32, the given token of each row, or NULL (no logprob wanted)
- *   temperature      finite, > 0
+ *   temperature      1e-4 to 1e4
  *   top_k            number of alternatives, 0 to 256
  *   out_stats        [rows] dls_token_stats
  *   out_top_ids      [rows, top_k] int32, by falling logit, equal ones by rising id
@@ -423,7 +423,7 @@ typedef struct dls_teacher {
   const float *values;   /* [rows, k] device, finite or -inf */
   int32_t k;             /* 1 to 256 */
   uint32_t flags;        /* DLS_TEACHER_LOGPROBS or 0 */
-  float temperature;     /* T, finite, > 0 */
+  float temperature;     /* T, 1e-4 to 1e4 */
   uint32_t reserved;     /* 0 */
 } dls_teacher;
 

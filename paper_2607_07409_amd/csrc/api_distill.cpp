@@ -30,8 +30,7 @@ dls_status check_stride(int64_t stride, int32_t V, const char* name) {
 }
 
 dls_status check_temperature(float t) {
-  // 1 / T and log2(e) / T have to be finite and not 0
-  if (!(t >= 1e-30f && t <= 1e30f)) return fail(DLS_ERR_ARG, "temperature %g outside [1e-30, 1e30]", (double)t);
+  if (!(t >= 1e-4f && t <= 1e4f)) return fail(DLS_ERR_ARG, "temperature %g outside [1e-4, 1e4]", (double)t);
   return DLS_OK;
 }
 

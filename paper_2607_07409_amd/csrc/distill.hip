@@ -49,7 +49,15 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__
     const float x = to_f32(row[v]);
     row_fold<1, false>(a, &x, x, te.c);
   });
-  row_chunks(row, g, [&](int, const float* x, float cm) { row_fold<N, false>(a, x, cm, te.c); }, [](int) {});
+  row_chunks(
+      row, g,
+      [&](int, const uint4* raw, auto n) {
+        float x[N * n];
+#pragma unroll
+        for (int u = 0; u < n; ++u) Chunk<T>::widen(raw[u], x + u * N);
+        row_fold<N * n, false>(a, x, max_of<N * n>(x), te.c);
+      },
+      [](int) {});
   a = row_block_merge<false>(a, shr);
   if (parts == 1) finish_row(row, V, r, a, te, sht, o);
   else if (threadIdx.x == 0) part_sums[(size_t)r * parts + part] = make_float2(a.R, a.s);

@@ -17,8 +17,6 @@
 // rows directly, in float32.  Their part of d_W is summed in k_head_w: the entries are put in order of the vocabulary
 // tile by a stable counting sort (so the sum's order, and every bit, is the same in every run) and streamed after the
 // rows as further tiles of Y, with their coefficients as two bf16 terms.
-#include <type_traits>
-
 #include "teacher.hpp"
 
 namespace dls {
@@ -417,20 +415,6 @@ __device__ __forceinline__ float4 widen4(uint2 v) {
   return make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
 }
 
-// sum over the 64 lanes, in every lane, without the LDS
-__device__ __forceinline__ float wave_total(float v) {
-  auto dpp = [&](auto ctrl) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  v += dpp(std::integral_constant<int, 0xB1>{});    // lane ^ 1
-  v += dpp(std::integral_constant<int, 0x4E>{});    // lane ^ 2
-  v += dpp(std::integral_constant<int, 0x141>{});   // the other half of eight
-  v += dpp(std::integral_constant<int, 0x140>{});   // the other half of sixteen
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
 __device__ __forceinline__ void add4(float4& d, float f, float4 y) {
   d.x = __builtin_fmaf(f, y.x, d.x);
   d.y = __builtin_fmaf(f, y.y, d.y);
@@ -486,7 +470,7 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
     for (int u = 0; u < 4; ++u)
       dot[u] = __builtin_fmaf(x.x, y[u].x, x.y * y[u].y) + __builtin_fmaf(x.z, y[u].z, x.w * y[u].w);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) dot[u] = wave_total(dot[u]);
+    for (int u = 0; u < 4; ++u) dot[u] = lanes_sum(dot[u]);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int k = k0 + u * kWaves;

@@ -8,6 +8,8 @@
 // all in float32, so that log-sum-exp = ln2 (R + log2 s), log p = ln2 (y - R - log2 s) and H = ln2 (log2 s - t / s).
 // One fused multiply-add forms y - R with a single rounding, whatever the size of R.
 #pragma once
+#include <type_traits>
+
 #include "dels_internal.hpp"
 #include "stream_load.hpp"
 
@@ -16,10 +18,40 @@ namespace dls {
 constexpr int kRowThreads = 256;
 constexpr int kRowUnroll = 2;             // chunks per thread and iteration
 constexpr float kNoRef = -2.0e38f;        // R before the first entry (finite: no inf - inf)
-constexpr float kPlainRef = 0x1p100f;     // |R| below this: y - R is formed by one fma
+constexpr float kPlainRef = 0x1p80f;      // |R| below this: y - R is formed by one fma
 constexpr float kMostY = 1.0e38f;         // entries beyond it count as it (only where no entry of the row is plain)
 constexpr float kLog2eLow = 1.92596299e-8f;   // log2(e) - kLog2e
 constexpr float kNoTerm = -1500.f;        // 2^kNoTerm = 0: a lower exponent adds nothing to s or t
+
+// Reductions over groups of W lanes (a power of two), in a fixed order, the result in every lane: by lane permutations of
+// the vector unit, not through the LDS
+template <int W, typename Op>
+__device__ __forceinline__ float lanes_reduce(float v, Op op) {
+  auto dpp = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if constexpr (W >= 2) v = op(v, dpp(std::integral_constant<int, 0xB1>{}));     // lane ^ 1
+  if constexpr (W >= 4) v = op(v, dpp(std::integral_constant<int, 0x4E>{}));     // lane ^ 2
+  if constexpr (W >= 8) v = op(v, dpp(std::integral_constant<int, 0x141>{}));    // the other half of eight
+  if constexpr (W >= 16) v = op(v, dpp(std::integral_constant<int, 0x140>{}));   // the other half of sixteen
+  if constexpr (W >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  if constexpr (W >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  return v;
+}
+template <int W = 64>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return lanes_reduce<W>(v, [](float a, float b) { return a + b; });
+}
+template <int W = 64>
+__device__ __forceinline__ float lanes_max(float v) {
+  return lanes_reduce<W>(v, [](float a, float b) { return fmaxf(a, b); });
+}
 
 struct RowSum {
   float R, s, t;
@@ -41,28 +73,50 @@ __device__ __forceinline__ void row_rescale(RowSum& a, float R) {
   a.R = R;
 }
 
+// The reference moves only where an entry passes it by kLazy, so that after a row's first entries hardly any wave
+// rescales: exponentials of up to 2^kLazy are as exact as others.
+constexpr float kLazy = 8.f;
+
+template <int n, bool ENT, bool FINITE>
+__device__ __forceinline__ void row_add(RowSum& a, const float* x, float c) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const float y = __builtin_fmaf(x[i], c, -a.R);   // -inf for a masked entry
+    const float e = fast_exp2(y);
+    a.s += e;
+    if (ENT) a.t = __builtin_fmaf(e, FINITE ? y : fmaxf(y, kNoTerm), a.t);
+  }
+}
+// the same where the reference moves, or is none yet, or lies far from any logit
+template <int n, bool ENT>
+__device__ __forceinline__ void row_add_moved(RowSum& a, const float* x, float cm, float c) {
+  if (cm > -INFINITY) row_rescale<ENT>(a, fmaxf(a.R, __builtin_amdgcn_fmed3f(cm * c, -kMostY, kMostY)));
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const float y = above_ref(x[i], c, a.R), e = fast_exp2(y);
+    a.s += e;
+    if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
+  }
+}
 // n entries whose largest is cm
 template <int n, bool ENT>
 __device__ __forceinline__ void row_fold(RowSum& a, const float* x, float cm, float c) {
-  const float R = fmaxf(a.R, cm * c);
-  if (fabsf(R) < kPlainRef) {
-    row_rescale<ENT>(a, R);
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const float y = __builtin_fmaf(x[i], c, -R);   // <= 0 up to rounding; -inf for a masked entry
-      const float e = fast_exp2(y);
-      a.s += e;
-      if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
-    }
-  } else if (cm > -INFINITY) {   // nothing plain so far, here neither
-    row_rescale<ENT>(a, fmaxf(a.R, __builtin_amdgcn_fmed3f(cm * c, -kMostY, kMostY)));
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const float y = above_ref(x[i], c, a.R), e = fast_exp2(y);
-      a.s += e;
-      if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
-    }
+  const bool move = cm * c > a.R + kLazy || a.R < -kPlainRef;
+  if (__builtin_amdgcn_ballot_w64(move) && move) {
+    row_add_moved<n, ENT>(a, x, cm, c);
+    return;
   }
+  row_add<n, ENT, false>(a, x, c);
+}
+
+// A piece with its masked entries (-inf, and whatever is as far below any logit) raised to a finite value that adds as
+// little, in the half words as they are: their order as unsigned numbers is that of the magnitudes.  The entropy's sum then
+// needs no test.  -2^96 c is finite and below -2^82 for every temperature within the limits.
+constexpr float kMasked = -0x1p96f;
+__device__ __forceinline__ uint4 raise_masked(uint4 v) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  const u16x8 most = (u16x8)(unsigned short)0xEF80;   // kMasked
+  return __builtin_bit_cast(uint4, __builtin_elementwise_min(__builtin_bit_cast(u16x8, v), most));
 }
 
 template <bool ENT>
@@ -76,15 +130,9 @@ __device__ __forceinline__ RowSum row_merge(RowSum a, RowSum b) {
 // over groups of W lanes, the same in every lane: the largest reference first, then one rescale and a sum
 template <bool ENT, int W = 64>
 __device__ __forceinline__ RowSum row_wave_merge(RowSum a) {
-  float R = a.R;
-#pragma unroll
-  for (int k = W / 2; k >= 1; k >>= 1) R = fmaxf(R, __shfl_xor(R, k));
-  row_rescale<ENT>(a, R);
-#pragma unroll
-  for (int k = W / 2; k >= 1; k >>= 1) {
-    a.s += __shfl_xor(a.s, k);
-    if (ENT) a.t += __shfl_xor(a.t, k);
-  }
+  row_rescale<ENT>(a, lanes_max<W>(a.R));
+  a.s = lanes_sum<W>(a.s);
+  if (ENT) a.t = lanes_sum<W>(a.t);
   return a;
 }
 
@@ -150,8 +198,9 @@ __device__ __forceinline__ float max_of(const float* x) {
   return m;
 }
 
-// Every chunk of the range through `fold(chunk, entries, largest)`, iteration by iteration; `pass(iteration)` after
-// each.  Loads run an iteration ahead (chunks past the range clamped to its last: loaded, never folded).
+// Every chunk of the range through `fold(chunk, raw, n)`, n chunks at a time: kRowUnroll chunks, kRowThreads apart, in
+// every whole iteration, single ones in the last; `pass(iteration)` after each iteration.  Loads run an iteration ahead
+// (chunks past the range clamped to its last: loaded, never folded).
 template <typename T, typename Fold, typename Pass>
 __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold fold, Pass pass) {
   constexpr int N = Chunk<T>::N, NT = kRowThreads;
@@ -167,14 +216,12 @@ __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u)
       next[u] = stream_load16(base + (size_t)min(b + t + (kRowUnroll + u) * NT, last) * N);
+    if (b + NT * kRowUnroll <= r.c1) {
+      fold(b + t, raw, std::integral_constant<int, kRowUnroll>{});
+    } else {
 #pragma unroll
-    for (int u = 0; u < kRowUnroll; ++u) {
-      const int c = b + t + u * NT;
-      if (c < r.c1) {
-        float x[N];
-        Chunk<T>::widen(raw[u], x);
-        fold(c, x, max_of<N>(x));
-      }
+      for (int u = 0; u < kRowUnroll; ++u)
+        if (b + t + u * NT < r.c1) fold(b + t + u * NT, raw + u, std::integral_constant<int, 1>{});
     }
     pass(it);
 #pragma unroll

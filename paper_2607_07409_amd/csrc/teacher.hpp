@@ -16,25 +16,21 @@ struct TeacherShared {
 };
 
 // sum (or maximum) over a workgroup of NT threads, in a fixed order, in every thread
-template <int NT, typename Op>
-__device__ __forceinline__ float block_reduce(float v, float* red, Op op) {
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) v = op(v, __shfl_xor(v, k));
+template <int NT>
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  v = lanes_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = red[threadIdx.x % (NT / 64)];
-#pragma unroll
-  for (int k = NT / 128; k >= 1; k >>= 1) v = op(v, __shfl_xor(v, k));
-  return v;
-}
-template <int NT>
-__device__ __forceinline__ float block_sum(float v, float* red) {
-  return block_reduce<NT>(v, red, [](float a, float b) { return a + b; });
+  return lanes_sum<NT / 64>(red[threadIdx.x % (NT / 64)]);
 }
 template <int NT>
 __device__ __forceinline__ float block_max(float v, float* red) {
-  return block_reduce<NT>(v, red, [](float a, float b) { return fmaxf(a, b); });
+  v = lanes_max(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return lanes_max<NT / 64>(red[threadIdx.x % (NT / 64)]);
 }
 
 // This thread's entry of row r as it is stored: id -1 and -inf for an absent one.

@@ -6,7 +6,8 @@
 // below: k blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.
 // Only the k best blocks are read again (from the caches), their entries at or above the bound are collected in LDS,
 // and the k best of those are put in order.  Nothing in the pass depends on the data, so a row of equal entries costs
-// what any other does.
+// what any other does.  The first selections need not be exact: a few blocks more than k come along where that saves a
+// digit of their keys.
 //
 // Keys: a value's bits as an integer of the same order in the upper half, the complement of the index (or chunk) in
 // the lower, so that the larger key is the better entry, ties going to the lower index, and no two are equal.  0 is
@@ -42,10 +43,11 @@ struct Select {
   int count;
 };
 
-// The k-th largest of the workgroup's keys (a bound that exactly k keys reach), or 1 where there are fewer than k;
-// `each(f)` calls f with every key of this thread.  Digit by digit from the top, until a digit's keys are all wanted.
+// A bound that at least k and at most `most` (>= k) of the workgroup's keys reach, or 1 where there are fewer than k;
+// `each(f)` calls f with every key of this thread.  Digit by digit from the top: with most = k to the k-th largest itself
+// (no two keys are equal), otherwise as soon as a digit's keys may all come along.
 template <typename Each>
-__device__ u64 kth_key(Each each, int k, Select& sh) {
+__device__ u64 bound_key(Each each, int k, int most, Select& sh) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   u64 prefix = 0;
   uint32_t need = (uint32_t)k;
@@ -57,23 +59,25 @@ __device__ u64 kth_key(Each each, int k, Select& sh) {
     });
     __syncthreads();
     const uint32_t h = sh.hist[t];   // thread t owns digit t
-    uint32_t from = h;               // keys with a digit of at least t
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_down(from, d);
-      if (lane + d < 64) from += o;
-    }
-    if (lane == 0) sh.wsum[wave] = from;
+    int from = (int)h;               // keys with a digit of at least t: within sixteen lanes, the wave, the workgroup
+    from += __builtin_amdgcn_update_dpp(0, from, 0x101, 0xf, 0xf, true);   // lane + 1, 2, 4, 8 of the sixteen
+    from += __builtin_amdgcn_update_dpp(0, from, 0x102, 0xf, 0xf, true);
+    from += __builtin_amdgcn_update_dpp(0, from, 0x104, 0xf, 0xf, true);
+    from += __builtin_amdgcn_update_dpp(0, from, 0x108, 0xf, 0xf, true);
+    const int r1 = __builtin_amdgcn_readlane(from, 16), r2 = __builtin_amdgcn_readlane(from, 32),
+              r3 = __builtin_amdgcn_readlane(from, 48);
+    from += (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
+    if (lane == 0) sh.wsum[wave] = (uint32_t)from;
     __syncthreads();
 #pragma unroll
     for (int w = 1; w < kThreads / 64; ++w)
-      if (w > wave) from += sh.wsum[w];
-    if (from >= need && from - h < need) {
+      if (w > wave) from += (int)sh.wsum[w];
+    if ((uint32_t)from >= need && (uint32_t)from - h < need) {
       sh.digit = (uint32_t)t;
-      sh.need = need - (from - h);
-      sh.whole = h == need - (from - h);
+      sh.need = need - ((uint32_t)from - h);
+      sh.whole = (uint32_t)k - need + (uint32_t)from <= (uint32_t)most;
     }
-    if (t == 0 && from < need) sh.digit = 256;
+    if (t == 0 && (uint32_t)from < need) sh.digit = 256;
     __syncthreads();
     if (sh.digit == 256) return 1;
     prefix = (prefix << 8) | sh.digit;
@@ -83,31 +87,34 @@ __device__ u64 kth_key(Each each, int k, Select& sh) {
   return 1;
 }
 
-// The k best of the keys that `each` gives, into out(rank, key), best first; missing ones as key 0.  `list` holds
-// kCand keys; at most k (<= 256) are ordered, each by the number of better ones.
+// keys list[0 .. n), n <= 256, into out(rank, key), best first, to rank k - 1; missing ones as key 0 (the list may hold
+// some, which come last)
+template <typename Out>
+__device__ __forceinline__ void order_keys(const u64* list, int n, int k, Out out) {
+  const int t = threadIdx.x;
+  if (t < n) {
+    const u64 mine = list[t];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += list[j] > mine || (list[j] == mine && j < t);
+    if (rank < k) out(rank, mine);
+  }
+  if (t >= n && t < k) out(t, (u64)0);
+}
+
+// the k (<= 256) best of the keys that `each` gives, in order; `list` holds 256
 template <typename Each, typename Out>
 __device__ void best_keys(Each each, int k, u64* list, Select& sh, Out out) {
   const int t = threadIdx.x;
-  const u64 bound = kth_key(each, k, sh);
+  const u64 bound = bound_key(each, k, 256, sh);
   __syncthreads();
   if (t == 0) sh.count = 0;
   __syncthreads();
   each([&](u64 key) {
-    if (key && key >= bound) {
-      const int at = atomicAdd(&sh.count, 1);
-      if (at < kCand) list[at] = key;
-    }
+    if (key && key >= bound) list[atomicAdd(&sh.count, 1)] = key;   // at most 256
   });
   __syncthreads();
-  const int n = min(sh.count, k);
-  if (t < n) {
-    const u64 mine = list[t];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > mine;
-    out(rank, mine);
-  } else if (t < k) {
-    out(t, (u64)0);
-  }
+  order_keys(list, sh.count, k, out);
 }
 
 struct RowOut {
@@ -171,13 +178,30 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
     const float x = to_f32(row[v]);
     row_fold<1, true>(a, &x, x, o.c);
   });
+  auto seen = [&](float cm, int chunk) {
+    bc = cm > bm ? chunk : bc;
+    bm = fmaxf(bm, cm);
+  };
   row_chunks(
       row, g,
-      [&](int c, const float* x, float cm) {
-        row_fold<N, true>(a, x, cm, o.c);
-        if (TOP) {
-          bc = cm > bm ? c : bc;
-          bm = fmaxf(bm, cm);
+      [&](int c, const uint4* raw, auto n) {
+        // masked entries of bf16 rows raised: the plain case of row_fold, without its test; otherwise as they are
+        constexpr bool kRaise = sizeof(T) == 2;
+        float x[N * n], cm = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+          Chunk<T>::widen(kRaise ? raise_masked(raw[u]) : raw[u], x + u * N);
+          const float m = max_of<N>(x + u * N);
+          if (TOP) seen(m, c + u * NT);
+          cm = fmaxf(cm, m);
+        }
+        const bool move = cm * o.c > a.R + kLazy || a.R < -kPlainRef;
+        if (__builtin_amdgcn_ballot_w64(move) && move) {
+#pragma unroll
+          for (int u = 0; u < n; ++u) Chunk<T>::widen(raw[u], x + u * N);
+          row_add_moved<N * n, true>(a, x, max_of<N * n>(x), o.c);
+        } else {
+          row_add<N * n, true, kRaise>(a, x, o.c);
         }
       },
       [&](int it) {
@@ -193,15 +217,33 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   }
   if (!TOP) return;
 
-  // the k best blocks
-  const u64 bound = kth_key([&](auto f) {
+  // the k best blocks, or some more
+  const u64 bound = bound_key([&](auto f) {
     for (int i = t; i < segs * NT; i += NT) f(blocks[i]);
-  }, o.k, sh);
+  }, o.k, min(256, 2 * o.k + 16), sh);
+  auto put = [&](int rank, u64 key) {
+    if (parts == 1) put_best(o, r, a, rank, key);
+    else part_keys[((size_t)r * parts + part) * o.k + rank] = key;
+  };
+  if ((uint32_t)(bound >> 32) <= order_of(kMasked)) {
+    // Fewer than k blocks hold an entry that is not masked (or as low as if it were: the pass does not tell those apart):
+    // the k best of all entries, read again for every digit
+    best_keys([&](auto f) {
+      row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
+      for (int c = g.c0 + t; c < g.c1; c += NT) {
+        float x[N];
+        Chunk<T>::load(row + g.h0 + (size_t)c * N, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(key_of(x[i], g.h0 + c * N + i));
+      }
+    }, o.k, list, sh, put);
+    return;
+  }
   __syncthreads();
   if (t == 0) sh.count = 0;
   __syncthreads();
   for (int i = t; i < segs * NT; i += NT)
-    if (blocks[i] && blocks[i] >= bound) chosen[atomicAdd(&sh.count, 1)] = (uint16_t)i;   // at most k <= 256
+    if (blocks[i] && blocks[i] >= bound) chosen[atomicAdd(&sh.count, 1)] = (uint16_t)i;   // at most 256
   __syncthreads();
   const int nb = sh.count, units = per_seg * kRowUnroll;
   // their entries, and the row's edge entries, as keys
@@ -229,24 +271,14 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   });
   __syncthreads();
   const int n = sh.count;
-  auto put = [&](int rank, u64 key) {
-    if (parts == 1) put_best(o, r, a, rank, key);
-    else part_keys[((size_t)r * parts + part) * o.k + rank] = key;
-  };
-  if (n > kCand) {   // too many at or above the bound (k blocks that hold most of the row's large entries)
-    best_keys(entries, o.k, list, sh, put);
-  } else if (n > o.k) {
-    __shared__ u64 best[256];
+  if (n <= 256) {
+    order_keys(list, n, o.k, put);
+  } else if (n <= kCand) {
     best_keys([&](auto f) {
       for (int i = t; i < n; i += NT) f(list[i]);
-    }, o.k, best, sh, put);
-  } else if (t < n) {
-    const u64 mine = list[t];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > mine;
-    put(rank, mine);
-  } else if (t < o.k) {
-    put(t, (u64)0);
+    }, o.k, blocks, sh, put);   // (the blocks have served)
+  } else {   // too many at or above the bound (k blocks that hold most of the row's large entries)
+    best_keys(entries, o.k, list, sh, put);
   }
 }
 
@@ -257,9 +289,12 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
                                                              const u64* __restrict__ part_keys) {
   __shared__ RowShared<> shr;
   __shared__ Select sh;
-  __shared__ u64 list[TOP ? kCand : 1];
+  __shared__ u64 list[TOP ? 256 : 1];
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x;
+  const u64* keys = part_keys + (size_t)r * parts * o.k;
+  const int n = parts * o.k;
+  if (TOP && n <= 256 && t < n) list[t] = keys[t];   // (row_block_merge's barrier comes before it is read)
   RowSum a = row_empty();
   if (t < parts) {   // parts <= 256
     const float4 p = part_sums[(size_t)r * parts + t];
@@ -268,11 +303,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
   a = row_block_merge<true>(a, shr);
   if (t == 0) put_stats(o, L + (size_t)r * stride, V, r, a);
   if (!TOP) return;
-  const u64* keys = part_keys + (size_t)r * parts * o.k;
-  const int n = parts * o.k;
-  best_keys([&](auto f) {
-    for (int i = t; i < n; i += kThreads) f(keys[i]);
-  }, o.k, list, sh, [&](int rank, u64 key) { put_best(o, r, a, rank, key); });
+  auto put = [&](int rank, u64 key) { put_best(o, r, a, rank, key); };
+  if (n <= 256)
+    order_keys(list, n, o.k, put);
+  else
+    best_keys([&](auto f) {
+      for (int i = t; i < n; i += kThreads) f(keys[i]);
+    }, o.k, list, sh, put);
 }
 
 // With alternatives wanted, a merge reads parts x k keys: at most about 2,048 of them

@@ -34,7 +34,7 @@ __device__ __forceinline__ void finish_row(const T* row, int V, int64_t r, const
   }
 }
 
-template <typename T>
+template <typename T, int U>
 __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__ L, int V, int64_t stride, TeacherArgs te,
                                                            float2* __restrict__ part_sums, LossOut o) {
   constexpr int N = Chunk<T>::N;
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__
     const float x = to_f32(row[v]);
     row_fold<1, false>(a, &x, x, te.c);
   });
-  row_chunks(
+  row_chunks<U>(
       row, g,
       [&](int, const uint4* raw, auto n) {
         float x[N * n];
@@ -331,7 +331,9 @@ hipError_t launch_loss_t(const DistillArgs& a, hipStream_t st) {
   float2* sums = rows + a.rows;
   const LossOut o = {a.out_loss, a.out_lse, a.grad ? rows : nullptr};
   const T* L = (const T*)a.logits;
-  k_distill_part<T><<<dim3((unsigned)a.rows, (unsigned)parts), kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, sums, o);
+  // whole rows: few workgroups a CU, so four loads a thread in flight instead of two
+  const auto part = parts == 1 ? k_distill_part<T, 4> : k_distill_part<T, 2>;
+  part<<<dim3((unsigned)a.rows, (unsigned)parts), kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, sums, o);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (parts > 1) {

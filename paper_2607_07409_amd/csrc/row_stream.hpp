@@ -16,7 +16,6 @@
 namespace dls {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowUnroll = 2;             // chunks per thread and iteration
 constexpr float kNoRef = -2.0e38f;        // R before the first entry (finite: no inf - inf)
 constexpr float kPlainRef = 0x1p80f;      // |R| below this: y - R is formed by one fma
 constexpr float kMostY = 1.0e38f;         // entries beyond it count as it (only where no entry of the row is plain)
@@ -198,41 +197,41 @@ __device__ __forceinline__ float max_of(const float* x) {
   return m;
 }
 
-// Every chunk of the range through `fold(chunk, raw, n)`, n chunks at a time: kRowUnroll chunks, kRowThreads apart, in
-// every whole iteration, single ones in the last; `pass(iteration)` after each iteration.  Loads run an iteration ahead
+// Every chunk of the range through `fold(chunk, raw, n)`, n chunks at a time: U chunks, kRowThreads apart, in every
+// whole iteration, single ones in the last; `pass(iteration)` after each iteration.  Loads run an iteration ahead
 // (chunks past the range clamped to its last: loaded, never folded).
-template <typename T, typename Fold, typename Pass>
+template <int U, typename T, typename Fold, typename Pass>
 __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold fold, Pass pass) {
   constexpr int N = Chunk<T>::N, NT = kRowThreads;
   if (r.c1 <= r.c0) return;
   const int t = threadIdx.x, last = r.c1 - 1;
   const T* base = row + r.h0;
-  uint4 raw[kRowUnroll];
+  uint4 raw[U];
 #pragma unroll
-  for (int u = 0; u < kRowUnroll; ++u) raw[u] = stream_load16(base + (size_t)min(r.c0 + t + u * NT, last) * N);
+  for (int u = 0; u < U; ++u) raw[u] = stream_load16(base + (size_t)min(r.c0 + t + u * NT, last) * N);
   int it = 0;
-  for (int b = r.c0; b < r.c1; b += NT * kRowUnroll, ++it) {
-    uint4 next[kRowUnroll];
+  for (int b = r.c0; b < r.c1; b += NT * U, ++it) {
+    uint4 next[U];
 #pragma unroll
-    for (int u = 0; u < kRowUnroll; ++u)
-      next[u] = stream_load16(base + (size_t)min(b + t + (kRowUnroll + u) * NT, last) * N);
-    if (b + NT * kRowUnroll <= r.c1) {
-      fold(b + t, raw, std::integral_constant<int, kRowUnroll>{});
+    for (int u = 0; u < U; ++u)
+      next[u] = stream_load16(base + (size_t)min(b + t + (U + u) * NT, last) * N);
+    if (b + NT * U <= r.c1) {
+      fold(b + t, raw, std::integral_constant<int, U>{});
     } else {
 #pragma unroll
-      for (int u = 0; u < kRowUnroll; ++u)
+      for (int u = 0; u < U; ++u)
         if (b + t + u * NT < r.c1) fold(b + t + u * NT, raw + u, std::integral_constant<int, 1>{});
     }
     pass(it);
 #pragma unroll
-    for (int u = 0; u < kRowUnroll; ++u) raw[u] = next[u];
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
   }
 }
 
 // workgroups per row: about four per CU when rows are few, each range at least two chunks a thread
 inline int row_parts(int64_t rows, int32_t V, int elem_bytes) {
   const int64_t p = (1024 + rows - 1) / std::max<int64_t>(rows, 1);
-  const int64_t cap = V / (kRowThreads * kRowUnroll * (16 / elem_bytes));
+  const int64_t cap = V / (kRowThreads * 2 * (16 / elem_bytes));
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(p, cap), 256));
 }
 

@@ -43,61 +43,99 @@ struct Select {
   int count;
 };
 
+// Digit t's keys, and where thread t's digit is the one in which the need-th key from above lies: sh.digit, what is still
+// needed of it, and whether all of it may come along (`above` keys are better than any digit).  sh.digit = 256: too few.
+__device__ __forceinline__ void find_digit(uint32_t need, uint32_t above, uint32_t most, Select& sh) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const uint32_t h = sh.hist[t];
+  int from = (int)h;   // keys with a digit of at least t: within sixteen lanes, the wave, the workgroup
+  from += __builtin_amdgcn_update_dpp(0, from, 0x101, 0xf, 0xf, true);   // lane + 1, 2, 4, 8 of the sixteen
+  from += __builtin_amdgcn_update_dpp(0, from, 0x102, 0xf, 0xf, true);
+  from += __builtin_amdgcn_update_dpp(0, from, 0x104, 0xf, 0xf, true);
+  from += __builtin_amdgcn_update_dpp(0, from, 0x108, 0xf, 0xf, true);
+  const int r1 = __builtin_amdgcn_readlane(from, 16), r2 = __builtin_amdgcn_readlane(from, 32),
+            r3 = __builtin_amdgcn_readlane(from, 48);
+  from += (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
+  if (lane == 0) sh.wsum[wave] = (uint32_t)from;
+  __syncthreads();
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w)
+    if (w > wave) from += (int)sh.wsum[w];
+  if ((uint32_t)from >= need && (uint32_t)from - h < need) {
+    sh.digit = (uint32_t)t;
+    sh.need = need - ((uint32_t)from - h);
+    sh.whole = above + (uint32_t)from <= most;
+  }
+  if (t == 0 && (uint32_t)from < need) sh.digit = 256;
+  __syncthreads();
+}
+
 // A bound that at least k and at most `most` (>= k) of the workgroup's keys reach, or 1 where there are fewer than k;
-// `each(f)` calls f with every key of this thread.  Digit by digit from the top: with most = k to the k-th largest itself
-// (no two keys are equal), otherwise as soon as a digit's keys may all come along.
+// `each(f)` calls f with every key of this thread.  No two keys are equal, so with most = k it is the k-th largest.
+// The first look counts the upper sixteen bits of the values from the largest down, 256 of them: two octaves in steps of
+// a bf16's last place, which is nearly always enough.  Then, or where the k-th lies lower, digit by digit.
 template <typename Each>
 __device__ u64 bound_key(Each each, int k, int most, Select& sh) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x;
+  uint32_t top = 0;
+  each([&](u64 key) { top = max(top, (uint32_t)(key >> 48)); });
+  top = (uint32_t)lanes_max((float)top);   // (sixteen bits: exact)
+  sh.hist[t] = 0;
+  __syncthreads();   // (and nobody reads wsum any more)
+  if ((t & 63) == 0) sh.wsum[t >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) top = max(top, sh.wsum[w]);
+  each([&](u64 key) {
+    if (key) atomicAdd(&sh.hist[255 - min(top - (uint32_t)(key >> 48), 255u)], 1u);
+  });
+  __syncthreads();
+  find_digit((uint32_t)k, 0, (uint32_t)most, sh);
+  if (sh.digit == 256) return 1;
   u64 prefix = 0;
   uint32_t need = (uint32_t)k;
-  for (int shift = 56; shift >= 0; shift -= 8) {
+  int shift = 56;
+  if (sh.digit > 0) {
+    prefix = top - (255 - sh.digit);
+    need = sh.need;
+    if (sh.whole) return prefix << 48;
+    shift = 40;
+  }
+  for (; shift >= 0; shift -= 8) {
+    __syncthreads();
     sh.hist[t] = 0;
     __syncthreads();
     each([&](u64 key) {
       if (key && (shift == 56 || (key >> (shift + 8)) == prefix)) atomicAdd(&sh.hist[(key >> shift) & 255], 1u);
     });
     __syncthreads();
-    const uint32_t h = sh.hist[t];   // thread t owns digit t
-    int from = (int)h;               // keys with a digit of at least t: within sixteen lanes, the wave, the workgroup
-    from += __builtin_amdgcn_update_dpp(0, from, 0x101, 0xf, 0xf, true);   // lane + 1, 2, 4, 8 of the sixteen
-    from += __builtin_amdgcn_update_dpp(0, from, 0x102, 0xf, 0xf, true);
-    from += __builtin_amdgcn_update_dpp(0, from, 0x104, 0xf, 0xf, true);
-    from += __builtin_amdgcn_update_dpp(0, from, 0x108, 0xf, 0xf, true);
-    const int r1 = __builtin_amdgcn_readlane(from, 16), r2 = __builtin_amdgcn_readlane(from, 32),
-              r3 = __builtin_amdgcn_readlane(from, 48);
-    from += (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
-    if (lane == 0) sh.wsum[wave] = (uint32_t)from;
-    __syncthreads();
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w)
-      if (w > wave) from += (int)sh.wsum[w];
-    if ((uint32_t)from >= need && (uint32_t)from - h < need) {
-      sh.digit = (uint32_t)t;
-      sh.need = need - ((uint32_t)from - h);
-      sh.whole = (uint32_t)k - need + (uint32_t)from <= (uint32_t)most;
-    }
-    if (t == 0 && (uint32_t)from < need) sh.digit = 256;
-    __syncthreads();
-    if (sh.digit == 256) return 1;
+    find_digit(need, (uint32_t)k - need, (uint32_t)most, sh);
     prefix = (prefix << 8) | sh.digit;
     need = sh.need;
-    if (sh.whole || shift == 0) return prefix << shift;
+    if (sh.whole) return prefix << shift;
   }
-  return 1;
+  return prefix;
 }
 
-// keys list[0 .. n), n <= 256, into out(rank, key), best first, to rank k - 1; missing ones as key 0 (the list may hold
-// some, which come last)
+// a place without a key, as a key below every entry's, no two alike
+__device__ __forceinline__ u64 no_key(int place) { return (u64)place + 1; }
+__device__ __forceinline__ bool is_entry(u64 key) { return key >> 32; }
+
+// keys list[0 .. n), n <= 256, into out(rank, key), best first, to rank k - 1; missing ones as key 0 (no_key's come last)
 template <typename Out>
 __device__ __forceinline__ void order_keys(const u64* list, int n, int k, Out out) {
   const int t = threadIdx.x;
   if (t < n) {
     const u64 mine = list[t];
-    int rank = 0;
+    int rank = 0, j = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += list[j] > mine || (list[j] == mine && j < t);
-    if (rank < k) out(rank, mine);
+    for (; j + 1 < n; j += 2) {
+      const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(list + j);
+      rank += two.x > mine;
+      rank += two.y > mine;
+    }
+    if (j < n) rank += list[j] > mine;
+    if (rank < k) out(rank, is_entry(mine) ? mine : 0);
   }
   if (t >= n && t < k) out(t, (u64)0);
 }
@@ -106,7 +144,7 @@ __device__ __forceinline__ void order_keys(const u64* list, int n, int k, Out ou
 template <typename Each, typename Out>
 __device__ void best_keys(Each each, int k, u64* list, Select& sh, Out out) {
   const int t = threadIdx.x;
-  const u64 bound = bound_key(each, k, 256, sh);
+  const u64 bound = bound_key(each, k, min(256, 2 * k + 16), sh);
   __syncthreads();
   if (t == 0) sh.count = 0;
   __syncthreads();
@@ -116,6 +154,7 @@ __device__ void best_keys(Each each, int k, u64* list, Select& sh, Out out) {
   __syncthreads();
   order_keys(list, sh.count, k, out);
 }
+constexpr int kOrderAll = 64;   // so many are put in order without looking for the best of them first
 
 struct RowOut {
   const int32_t* tokens;
@@ -151,21 +190,21 @@ __device__ __forceinline__ void put_best(const RowOut& o, int64_t r, const RowSu
   o.logprobs[at] = key ? log_p(o, a, value_of(key), fast_log2(a.s)) : -INFINITY;
 }
 
-template <typename T, bool TOP>
+template <typename T, bool TOP, int U>
 __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict__ L, int V, int64_t stride, RowOut o,
                                                             int segs, float4* __restrict__ part_sums,
                                                             u64* __restrict__ part_keys) {
   constexpr int N = Chunk<T>::N, NT = kThreads;
   __shared__ RowShared<> shr;
   __shared__ Select sh;
-  __shared__ u64 blocks[TOP ? kMostSegs * NT : 1];
-  __shared__ u64 list[TOP ? kCand : 1];
+  __shared__ __attribute__((aligned(16))) u64 blocks[TOP ? kMostSegs * NT : 1];
+  __shared__ __attribute__((aligned(16))) u64 list[TOP ? kCand : 1];
   __shared__ uint16_t chosen[256];
   const int part = blockIdx.y, parts = gridDim.y, t = threadIdx.x;
   const int64_t r = blockIdx.x;
   const T* row = L + (size_t)r * stride;
   const RowRange g = row_range(row, V, part, parts);
-  const int iters = (g.c1 - g.c0 + NT * kRowUnroll - 1) / (NT * kRowUnroll);
+  const int iters = (g.c1 - g.c0 + NT * U - 1) / (NT * U);
   const int per_seg = max(1, (iters + segs - 1) / segs);   // iterations per block
 
   RowSum a = row_empty();
@@ -182,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
     bc = cm > bm ? chunk : bc;
     bm = fmaxf(bm, cm);
   };
-  row_chunks(
+  row_chunks<U>(
       row, g,
       [&](int c, const uint4* raw, auto n) {
         // masked entries of bf16 rows raised: the plain case of row_fold, without its test; otherwise as they are
@@ -245,13 +284,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   for (int i = t; i < segs * NT; i += NT)
     if (blocks[i] && blocks[i] >= bound) chosen[atomicAdd(&sh.count, 1)] = (uint16_t)i;   // at most 256
   __syncthreads();
-  const int nb = sh.count, units = per_seg * kRowUnroll;
+  const int nb = sh.count, units = per_seg * U;
   // their entries, and the row's edge entries, as keys
   auto entries = [&](auto f) {
     row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
     for (int w = t; w < nb * units; w += NT) {
       const int blk = chosen[w / units], j = w % units;
-      const int c = g.c0 + ((blk / NT) * per_seg * kRowUnroll + j) * NT + blk % NT;
+      const int c = g.c0 + ((blk / NT) * per_seg * U + j) * NT + blk % NT;
       if (c >= g.c1) continue;
       float x[N];
       Chunk<T>::load(row + g.h0 + (size_t)c * N, x);
@@ -271,7 +310,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   });
   __syncthreads();
   const int n = sh.count;
-  if (n <= 256) {
+  if (n <= kOrderAll) {
     order_keys(list, n, o.k, put);
   } else if (n <= kCand) {
     best_keys([&](auto f) {
@@ -289,12 +328,15 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
                                                              const u64* __restrict__ part_keys) {
   __shared__ RowShared<> shr;
   __shared__ Select sh;
-  __shared__ u64 list[TOP ? 256 : 1];
+  __shared__ __attribute__((aligned(16))) u64 list[TOP ? 256 : 1];
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x;
   const u64* keys = part_keys + (size_t)r * parts * o.k;
   const int n = parts * o.k;
-  if (TOP && n <= 256 && t < n) list[t] = keys[t];   // (row_block_merge's barrier comes before it is read)
+  if (TOP && n <= kOrderAll && t < n) {   // (row_block_merge's barrier comes before it is read)
+    const u64 key = keys[t];
+    list[t] = key ? key : no_key(t);
+  }
   RowSum a = row_empty();
   if (t < parts) {   // parts <= 256
     const float4 p = part_sums[(size_t)r * parts + t];
@@ -304,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
   if (t == 0) put_stats(o, L + (size_t)r * stride, V, r, a);
   if (!TOP) return;
   auto put = [&](int rank, u64 key) { put_best(o, r, a, rank, key); };
-  if (n <= 256)
+  if (n <= kOrderAll)
     order_keys(list, n, o.k, put);
   else
     best_keys([&](auto f) {
@@ -328,8 +370,10 @@ hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
   u64* keys = (u64*)(a.ws + l.off_keys);
   const int segs = a.k <= 32 ? 1 : kMostSegs;
   const T* L = (const T*)a.logits;
-  if (a.k > 0) k_logprobs_part<T, true><<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
-  else k_logprobs_part<T, false><<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
+  // whole rows: few workgroups a CU, so four loads a thread in flight instead of two
+  const auto part = a.k > 0 ? (parts == 1 ? k_logprobs_part<T, true, 4> : k_logprobs_part<T, true, 2>)
+                            : (parts == 1 ? k_logprobs_part<T, false, 4> : k_logprobs_part<T, false, 2>);
+  part<<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   if (a.k > 0) k_logprobs_merge<T, true><<<(unsigned)a.rows, kThreads, 0, st>>>(L, a.V, a.stride, o, parts, sums, keys);

@@ -189,12 +189,18 @@ __device__ __forceinline__ void row_edges(const RowRange& r, int V, int part, in
   if (part == parts - 1 && t < V - r.tail0) f(r.tail0 + t);
 }
 
+// (as an instruction: the compiler would first pass every loaded value through a maximum of its own, for signalling NaN)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+  return m;
+}
 template <int n>
 __device__ __forceinline__ float max_of(const float* x) {
   float m = x[0];
 #pragma unroll
-  for (int i = 1; i < n; ++i) m = fmaxf(m, x[i]);
-  return m;
+  for (int i = 1; i + 1 < n; i += 2) m = max3(m, x[i], x[i + 1]);
+  return n % 2 ? m : max3(m, x[n - 1], x[n - 1]);
 }
 
 // Every chunk of the range through `fold(chunk, raw, n)`, n chunks at a time: U chunks, kRowThreads apart, in every
@@ -202,19 +208,21 @@ __device__ __forceinline__ float max_of(const float* x) {
 // (chunks past the range clamped to its last: loaded, never folded).
 template <int U, typename T, typename Fold, typename Pass>
 __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold fold, Pass pass) {
-  constexpr int N = Chunk<T>::N, NT = kRowThreads;
+  constexpr int NT = kRowThreads;
   if (r.c1 <= r.c0) return;
-  const int t = threadIdx.x, last = r.c1 - 1;
-  const T* base = row + r.h0;
+  const int t = threadIdx.x;
+  const char* base = reinterpret_cast<const char*>(row + r.h0);   // one address, 32-bit offsets (a row is below 2^26 bytes)
+  const uint32_t last = (uint32_t)(r.c1 - 1) * 16;
+  uint32_t off = (uint32_t)(r.c0 + t) * 16;
   uint4 raw[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) raw[u] = stream_load16(base + (size_t)min(r.c0 + t + u * NT, last) * N);
+  for (int u = 0; u < U; ++u) raw[u] = stream_load16(base + min(off + u * NT * 16, last));
   int it = 0;
   for (int b = r.c0; b < r.c1; b += NT * U, ++it) {
     uint4 next[U];
+    off += U * NT * 16;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      next[u] = stream_load16(base + (size_t)min(b + t + (U + u) * NT, last) * N);
+    for (int u = 0; u < U; ++u) next[u] = stream_load16(base + min(off + u * NT * 16, last));
     if (b + NT * U <= r.c1) {
       fold(b + t, raw, std::integral_constant<int, U>{});
     } else {

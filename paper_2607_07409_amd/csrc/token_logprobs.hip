@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   });
   auto seen = [&](float cm, int chunk) {
     bc = cm > bm ? chunk : bc;
-    bm = fmaxf(bm, cm);
+    bm = max3(bm, cm, cm);
   };
   row_chunks<U>(
       row, g,
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
           Chunk<T>::widen(kRaise ? raise_masked(raw[u]) : raw[u], x + u * N);
           const float m = max_of<N>(x + u * N);
           if (TOP) seen(m, c + u * NT);
-          cm = fmaxf(cm, m);
+          cm = max3(cm, m, m);
         }
         const bool move = cm * o.c > a.R + kLazy || a.R < -kPlainRef;
         if (__builtin_amdgcn_ballot_w64(move) && move) {

@@ -203,32 +203,35 @@ __device__ __forceinline__ float max_of(const float* x) {
   return n % 2 ? m : max3(m, x[n - 1], x[n - 1]);
 }
 
-// Every chunk of the range through `fold(chunk, raw, n)`, n chunks at a time: U chunks, kRowThreads apart, in every
-// whole iteration, single ones in the last; `pass(iteration)` after each iteration.  Loads run an iteration ahead
-// (chunks past the range clamped to its last: loaded, never folded).
+// Every chunk of the range, in iterations of U chunks a thread: eight lanes have the 8 U chunks of one block, 128 bytes
+// of it at a load, so that a block is one stretch of memory and the blocks, numbered iteration by iteration, rise
+// along the row.  `fold(raw, n)` gets n chunks at a time, U in every whole iteration, single ones in the last;
+// `pass(iteration)` comes after each.  Loads run an iteration ahead (chunks past the range clamped to its last: loaded,
+// never folded).
+constexpr int kBlockLanes = 8;
 template <int U, typename T, typename Fold, typename Pass>
 __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold fold, Pass pass) {
   constexpr int NT = kRowThreads;
   if (r.c1 <= r.c0) return;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, mine = r.c0 + t / kBlockLanes * (kBlockLanes * U) + t % kBlockLanes;
   const char* base = reinterpret_cast<const char*>(row + r.h0);   // one address, 32-bit offsets (a row is below 2^26 bytes)
   const uint32_t last = (uint32_t)(r.c1 - 1) * 16;
-  uint32_t off = (uint32_t)(r.c0 + t) * 16;
+  uint32_t off = (uint32_t)mine * 16;
   uint4 raw[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) raw[u] = stream_load16(base + min(off + u * NT * 16, last));
+  for (int u = 0; u < U; ++u) raw[u] = stream_load16(base + min(off + u * kBlockLanes * 16, last));
   int it = 0;
   for (int b = r.c0; b < r.c1; b += NT * U, ++it) {
     uint4 next[U];
     off += U * NT * 16;
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = stream_load16(base + min(off + u * NT * 16, last));
+    for (int u = 0; u < U; ++u) next[u] = stream_load16(base + min(off + u * kBlockLanes * 16, last));
     if (b + NT * U <= r.c1) {
-      fold(b + t, raw, std::integral_constant<int, U>{});
+      fold(raw, std::integral_constant<int, U>{});
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (b + t + u * NT < r.c1) fold(b + t + u * NT, raw + u, std::integral_constant<int, 1>{});
+        if (mine + (b - r.c0) + u * kBlockLanes < r.c1) fold(raw + u, std::integral_constant<int, 1>{});
     }
     pass(it);
 #pragma unroll

@@ -1,15 +1,15 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits.
 //
-// One pass (row_stream.hpp) gives the log-sum-exp and the entropy.  The alternatives come out of the same pass: the
-// chunks that a thread folds are grouped into blocks, and of each block the pass keeps the largest entry's value and
-// chunk.  Ordered by (value, lower chunk first), the k-th of these block maxima bounds the row's k best entries from
-// below: k blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.
-// Only the k best blocks are read again (from the caches), their entries at or above the bound are collected in LDS,
-// and the k best of those are put in order.  Nothing in the pass depends on the data, so a row of equal entries costs
-// what any other does.  The first selections need not be exact: a few blocks more than k come along where that saves a
-// digit of their keys.
+// One pass (row_stream.hpp) gives the log-sum-exp and the entropy.  The alternatives come out of the same pass: eight
+// lanes' chunks of an iteration are one stretch of the row, a block, and of each block the pass keeps the largest entry.
+// Ordered by (value, lower block first), the k-th of these block maxima bounds the row's k best entries from below: k
+// blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.  Only the k
+// best blocks are read again (512 bytes each, from the caches), their entries at or above the bound are collected in
+// LDS, and the k best of those are put in order.  Nothing in the pass depends on the data, so a row of equal entries
+// costs what any other does.  The first selections need not be exact: a few blocks more than k come along where that
+// saves a look at their keys.
 //
-// Keys: a value's bits as an integer of the same order in the upper half, the complement of the index (or chunk) in
+// Keys: a value's bits as an integer of the same order in the upper half, the complement of the index (or block) in
 // the lower, so that the larger key is the better entry, ties going to the lower index, and no two are equal.  0 is
 // no key.  Masked entries (-inf) and NaN have none.
 #include "row_stream.hpp"
@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kThreads = kRowThreads;
 constexpr int kCand = 1024;       // candidates held in LDS; rows with more are selected from by re-reading them
-constexpr int kMostSegs = 4;      // blocks per thread
+constexpr int kBlocks = 1024;     // of a part: 32 iterations
 
 typedef unsigned long long u64;
 
@@ -192,48 +192,38 @@ __device__ __forceinline__ void put_best(const RowOut& o, int64_t r, const RowSu
 
 template <typename T, bool TOP, int U>
 __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict__ L, int V, int64_t stride, RowOut o,
-                                                            int segs, float4* __restrict__ part_sums,
+                                                            float4* __restrict__ part_sums,
                                                             u64* __restrict__ part_keys) {
   constexpr int N = Chunk<T>::N, NT = kThreads;
   __shared__ RowShared<> shr;
   __shared__ Select sh;
-  __shared__ __attribute__((aligned(16))) u64 blocks[TOP ? kMostSegs * NT : 1];
+  __shared__ __attribute__((aligned(16))) u64 blocks[TOP ? kBlocks : 1];
   __shared__ __attribute__((aligned(16))) u64 list[TOP ? kCand : 1];
   __shared__ uint16_t chosen[256];
   const int part = blockIdx.y, parts = gridDim.y, t = threadIdx.x;
   const int64_t r = blockIdx.x;
   const T* row = L + (size_t)r * stride;
   const RowRange g = row_range(row, V, part, parts);
-  const int iters = (g.c1 - g.c0 + NT * U - 1) / (NT * U);
-  const int per_seg = max(1, (iters + segs - 1) / segs);   // iterations per block
+  const int nblocks = (g.c1 - g.c0 + NT * U - 1) / (NT * U) * (NT / kBlockLanes);   // <= kBlocks
 
   RowSum a = row_empty();
-  float bm = -INFINITY;   // the block's largest value and its chunk, lowest chunk first
-  int bc = 0;
-  if (TOP)
-    for (int i = t; i < kMostSegs * NT; i += NT) blocks[i] = 0;
-  if (TOP) __syncthreads();
+  float bm = -INFINITY;   // the largest of this thread's chunks of an iteration
   row_edges(g, V, part, parts, [&](int v) {
     const float x = to_f32(row[v]);
     row_fold<1, true>(a, &x, x, o.c);
   });
-  auto seen = [&](float cm, int chunk) {
-    bc = cm > bm ? chunk : bc;
-    bm = max3(bm, cm, cm);
-  };
   row_chunks<U>(
       row, g,
-      [&](int c, const uint4* raw, auto n) {
+      [&](const uint4* raw, auto n) {
         // masked entries of bf16 rows raised: the plain case of row_fold, without its test; otherwise as they are
         constexpr bool kRaise = sizeof(T) == 2;
-        float x[N * n], cm = -INFINITY;
+        float x[N * n];
 #pragma unroll
         for (int u = 0; u < n; ++u) {
           Chunk<T>::widen(kRaise ? raise_masked(raw[u]) : raw[u], x + u * N);
-          const float m = max_of<N>(x + u * N);
-          if (TOP) seen(m, c + u * NT);
-          cm = max3(cm, m, m);
         }
+        const float cm = max_of<N * n>(x);
+        if (TOP) bm = max3(bm, cm, cm);
         const bool move = cm * o.c > a.R + kLazy || a.R < -kPlainRef;
         if (__builtin_amdgcn_ballot_w64(move) && move) {
 #pragma unroll
@@ -244,10 +234,11 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
         }
       },
       [&](int it) {
-        if (TOP && (it % per_seg == per_seg - 1 || it == iters - 1)) {
-          blocks[(it / per_seg) * NT + t] = key_of(bm, bc);
-          bm = -INFINITY;
-        }
+        if (!TOP) return;
+        const float m = lanes_max<kBlockLanes>(bm);
+        const int blk = it * (NT / kBlockLanes) + t / kBlockLanes;
+        if (t % kBlockLanes == 0) blocks[blk] = key_of(m, blk);
+        bm = -INFINITY;
       });
   a = row_block_merge<true>(a, shr);
   if (t == 0) {
@@ -258,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
 
   // the k best blocks, or some more
   const u64 bound = bound_key([&](auto f) {
-    for (int i = t; i < segs * NT; i += NT) f(blocks[i]);
+    for (int i = t; i < nblocks; i += NT) f(blocks[i]);
   }, o.k, min(256, 2 * o.k + 16), sh);
   auto put = [&](int rank, u64 key) {
     if (parts == 1) put_best(o, r, a, rank, key);
@@ -281,22 +272,21 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   __syncthreads();
   if (t == 0) sh.count = 0;
   __syncthreads();
-  for (int i = t; i < segs * NT; i += NT)
+  for (int i = t; i < nblocks; i += NT)
     if (blocks[i] && blocks[i] >= bound) chosen[atomicAdd(&sh.count, 1)] = (uint16_t)i;   // at most 256
   __syncthreads();
-  const int nb = sh.count, units = per_seg * U;
+  const int nb = sh.count;
   // their entries, and the row's edge entries, as keys
   auto entries = [&](auto f) {
     row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
-    for (int w = t; w < nb * units; w += NT) {
-      const int blk = chosen[w / units], j = w % units;
-      const int c = g.c0 + ((blk / NT) * per_seg * U + j) * NT + blk % NT;
+    for (int w = t; w < nb * (kBlockLanes * U); w += NT) {
+      const int blk = chosen[w / (kBlockLanes * U)], c = g.c0 + blk * (kBlockLanes * U) + w % (kBlockLanes * U);
       if (c >= g.c1) continue;
       float x[N];
       Chunk<T>::load(row + g.h0 + (size_t)c * N, x);
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (key_of(x[i], c) >= bound) f(key_of(x[i], g.h0 + c * N + i));
+        if (key_of(x[i], blk) >= bound) f(key_of(x[i], g.h0 + c * N + i));
     }
   };
   __syncthreads();
@@ -354,10 +344,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
     }, o.k, list, sh, put);
 }
 
-// With alternatives wanted, a merge reads parts x k keys: at most about 2,048 of them
+// With alternatives wanted, a merge reads parts x k keys, at most about 2,048 of them, and a part has at most kBlocks
+// blocks of four chunks a lane
 int logprobs_parts(int64_t rows, int32_t V, int elem_bytes, int k) {
   const int p = row_parts(rows, V, elem_bytes);
-  return k > 0 ? std::max(1, std::min(p, 2048 / k)) : p;
+  if (k == 0) return p;
+  const int most = kBlocks * kBlockLanes * 4 * (16 / elem_bytes);
+  return std::max(std::max(1, std::min(p, 2048 / k)), (V + most - 1) / most);
 }
 
 template <typename T>
@@ -368,12 +361,12 @@ hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
   const LogprobsLayout l = logprobs_layout(a.rows, a.V, (int)sizeof(T), a.k);
   float4* sums = (float4*)a.ws;
   u64* keys = (u64*)(a.ws + l.off_keys);
-  const int segs = a.k <= 32 ? 1 : kMostSegs;
   const T* L = (const T*)a.logits;
-  // whole rows: few workgroups a CU, so four loads a thread in flight instead of two
-  const auto part = a.k > 0 ? (parts == 1 ? k_logprobs_part<T, true, 4> : k_logprobs_part<T, true, 2>)
-                            : (parts == 1 ? k_logprobs_part<T, false, 4> : k_logprobs_part<T, false, 2>);
-  part<<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, segs, sums, keys);
+  // Long parts: few workgroups a CU, so four loads a thread in flight instead of two
+  const bool four = a.V / parts > 16384;
+  const auto part = a.k > 0 ? (four ? k_logprobs_part<T, true, 4> : k_logprobs_part<T, true, 2>)
+                            : (four ? k_logprobs_part<T, false, 4> : k_logprobs_part<T, false, 2>);
+  part<<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, sums, keys);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   if (a.k > 0) k_logprobs_merge<T, true><<<(unsigned)a.rows, kThreads, 0, st>>>(L, a.V, a.stride, o, parts, sums, keys);

@@ -149,6 +149,17 @@ def test_large_entries_in_few_blocks(dtype, per, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,V", [(BF16, 263001), (F32, 131101)])
+def test_rows_too_long_for_one_workgroup(dtype, V):
+    """As many rows as workgroups are wanted, and still parts: a part holds the maxima of 1,024 blocks."""
+    x = torch.zeros((1024, V), dtype=dtype, device="cuda")
+    x[:3] = _rows(3, V, dtype, 81)
+    x[1, V - 1], x[2, 0] = 30.0, 30.0
+    tok = _tokens(1024, V, 82)
+    _check(x, tok, 20, 1.0, B.token_logprobs(x, tok, top_k=20), rows=[0, 1, 2, 3, 1023])
+
+
+@pytest.mark.gpu
 def test_nan_and_infinite_entries_end():
     """Their results are not specified; ids stay in range and the other rows are untouched."""
     x, tok = _rows(4, 5003, F32, 31), _tokens(4, 5003, 32)

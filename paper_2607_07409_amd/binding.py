@@ -488,28 +488,32 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     if t.dim() != 2:
         raise ValueError(f"{name} must be [rows, V], got {tuple(t.shape)}")
     rows, V = t.shape
-    if V > 1 and t.stride(1) != 1:
+    step, entry = t.stride()
+    if V > 1 and entry != 1:
         raise ValueError(f"the entries of a row of {name} must be contiguous")
     if rows <= 1:
         return V
-    if t.stride(0) < V:
-        raise ValueError(f"the rows of {name} overlap (stride {t.stride(0)} < {V})")
-    return t.stride(0)
+    if step < V:
+        raise ValueError(f"the rows of {name} overlap (stride {step} < {V})")
+    return step
 
 
 def _vector(t: Optional[torch.Tensor], name: str, shape, dtype, device):
-    """The pointer of a dense tensor of the given shape and type on the given device (None passes)."""
+    """The address of a dense tensor of the given shape and type on the given device (None passes)."""
     if t is None:
         return None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+_here = contextlib.nullcontext()
 
 
 def _on(device: torch.device, stream):
@@ -523,15 +527,24 @@ def _on(device: torch.device, stream):
         return torch.cuda.stream(stream)
     if device.index != torch.cuda.current_device():
         return torch.cuda.device(device)
-    return contextlib.nullcontext()
+    return _here
 
 
-def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _scratch(workspace: Optional[torch.Tensor], need: int, device):
+    """(tensor, bytes) of the caller's workspace, or of one of its own."""
     if workspace is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        return (torch.empty(need, dtype=torch.uint8, device=device), need) if need else (None, 0)
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {device}")
-    return workspace
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _address(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_of(stream, device) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
 
 
 def token_logprobs_workspace_size(rows: int, V: int, top_k: int = 0) -> int:
@@ -544,22 +557,23 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     wider ones) at a temperature, with the row's entropy and log-sum-exp and its top_k most likely entries.
     tokens [rows] int32, or None.  Returns (stats [rows, 3] float32 with the fields LOGPROB_FIELDS, ids
     [rows, top_k] int32, logprobs [rows, top_k] float32); out: these three tensors, to be overwritten."""
-    dev = logits.device
-    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    dev, f32 = logits.device, torch.float32
     stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
-    k = max(top_k, 0)
+    (rows, V), k, L = logits.shape, max(top_k, 0), lib()
     with _on(dev, stream):
         if out is None:
-            out = (torch.empty((rows, 3), dtype=torch.float32, device=dev),
-                   torch.empty((rows, k), dtype=torch.int32, device=dev),
-                   torch.empty((rows, k), dtype=torch.float32, device=dev))
-        st, ids, lp = out
-        ws = _scratch(workspace, token_logprobs_workspace_size(rows, V, top_k), dev)
-        _check(lib().dls_token_logprobs(
-            _ptr(logits), dtype, rows, V, stride, _vector(tokens, "tokens", (rows,), torch.int32, dev), temperature, top_k,
-            _vector(st, "stats", (rows, 3), torch.float32, dev), _vector(ids, "ids", (rows, k), torch.int32, dev),
-            _vector(lp, "logprobs", (rows, k), torch.float32, dev), _ptr(ws), ws.numel() * ws.element_size(),
-            _stream(stream)))
+            st, ids = torch.empty((rows, 3), dtype=f32, device=dev), torch.empty((rows, k), dtype=torch.int32, device=dev)
+            lp = torch.empty((rows, k), dtype=f32, device=dev)
+            places = st.data_ptr(), ids.data_ptr(), lp.data_ptr()
+        else:
+            st, ids, lp = out
+            places = (_vector(st, "stats", (rows, 3), f32, dev), _vector(ids, "ids", (rows, k), torch.int32, dev),
+                      _vector(lp, "logprobs", (rows, k), f32, dev))
+        ws, size = _scratch(workspace, L.dls_token_logprobs_workspace_size(rows, V, top_k), dev)
+        status = L.dls_token_logprobs(logits.data_ptr(), dtype, rows, V, stride,
+                                      _vector(tokens, "tokens", (rows,), torch.int32, dev), temperature, top_k, *places,
+                                      _address(ws), size, _stream_of(stream, dev))
+    _check(status)
     return st, ids, lp
 
 
@@ -585,21 +599,24 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, 
     outside [0, V) or the value -inf are absent.  Returns (loss [rows], lse [rows], grad): with want_grad the
     gradient [rows, V] by the logits, each row weighted by grad_loss [rows] (None: 1), else None.  out: (loss, lse,
     grad) to be overwritten; grad may be `logits` itself."""
-    dev = logits.device
-    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    dev, f32 = logits.device, torch.float32
     stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
+    (rows, V), L = logits.shape, lib()
     with _on(dev, stream):
         if out is None:
-            out = (torch.empty(rows, dtype=torch.float32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev),
-                   torch.empty((rows, V), dtype=logits.dtype, device=dev) if want_grad else None)
-        loss, lse, grad = out
-        ws = _scratch(workspace, distill_workspace_size(rows, V), dev)
-        gptr, gstride = _grad_rows(grad, logits)
-        _check(lib().dls_distill_loss(
-            _ptr(logits), dtype, rows, V, stride, _teacher(ids, values, rows, temperature, renormalise, dev),
-            _vector(grad_loss, "grad_loss", (rows,), torch.float32, dev), _vector(loss, "loss", (rows,), torch.float32, dev),
-            _vector(lse, "lse", (rows,), torch.float32, dev), gptr, gstride, _ptr(ws), ws.numel() * ws.element_size(),
-            _stream(stream)))
+            loss, lse = torch.empty(rows, dtype=f32, device=dev), torch.empty(rows, dtype=f32, device=dev)
+            grad = torch.empty((rows, V), dtype=logits.dtype, device=dev) if want_grad else None
+            places = loss.data_ptr(), lse.data_ptr(), _address(grad), V
+        else:
+            loss, lse, grad = out
+            places = (_vector(loss, "loss", (rows,), f32, dev), _vector(lse, "lse", (rows,), f32, dev),
+                      *_grad_rows(grad, logits))
+        ws, size = _scratch(workspace, L.dls_distill_workspace_size(rows, V), dev)
+        status = L.dls_distill_loss(logits.data_ptr(), dtype, rows, V, stride,
+                                    _teacher(ids, values, rows, temperature, renormalise, dev),
+                                    _vector(grad_loss, "grad_loss", (rows,), f32, dev), *places, _address(ws), size,
+                                    _stream_of(stream, dev))
+    _check(status)
     return loss, lse, grad
 
 
@@ -608,7 +625,7 @@ def _grad_rows(grad: Optional[torch.Tensor], logits: torch.Tensor):
         return None, 0
     if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device:
         raise ValueError("the gradient must have the logits' shape, type and device")
-    return _ptr(grad), _row_stride(grad, "grad")
+    return grad.data_ptr(), _row_stride(grad, "grad")
 
 
 def distill_grad(logits: torch.Tensor, lse: torch.Tensor, ids: torch.Tensor, values: torch.Tensor,
@@ -616,17 +633,17 @@ def distill_grad(logits: torch.Tensor, lse: torch.Tensor, ids: torch.Tensor, val
                  stream=None) -> torch.Tensor:
     """Gradient of distill_loss by the logits, from the log-sum-exps [rows] that it returned, each row weighted by
     grad_loss [rows] (None: 1).  out: the tensor to be overwritten (may be `logits` itself)."""
-    dev = logits.device
-    rows, V = logits.shape if logits.dim() == 2 else (0, 0)
+    dev, f32 = logits.device, torch.float32
     stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
+    rows, V = logits.shape
     with _on(dev, stream):
         if out is None:
             out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
-        gptr, gstride = _grad_rows(out, logits)
-        _check(lib().dls_distill_grad(
-            _ptr(logits), dtype, rows, V, stride, _vector(lse, "lse", (rows,), torch.float32, dev),
-            _teacher(ids, values, rows, temperature, renormalise, dev),
-            _vector(grad_loss, "grad_loss", (rows,), torch.float32, dev), gptr, gstride, _stream(stream)))
+        status = lib().dls_distill_grad(logits.data_ptr(), dtype, rows, V, stride, _vector(lse, "lse", (rows,), f32, dev),
+                                        _teacher(ids, values, rows, temperature, renormalise, dev),
+                                        _vector(grad_loss, "grad_loss", (rows,), f32, dev), *_grad_rows(out, logits),
+                                        _stream_of(stream, dev))
+    _check(status)
     return out
 
 
@@ -643,7 +660,7 @@ def head_distill(rho: torch.Tensor, w_vocab: torch.Tensor, ids: torch.Tensor, va
     dev = rho.device
     if rho.dim() != 2 or w_vocab.dim() != 2:
         raise ValueError("rho must be [rows, r] and w_vocab [V, r]")
-    (rows, r), V = rho.shape, w_vocab.shape[0]
+    (rows, r), V, L = rho.shape, w_vocab.shape[0], lib()
     f32, bf16 = torch.float32, torch.bfloat16
     with _on(dev, stream):
         if out is None:
@@ -652,12 +669,14 @@ def head_distill(rho: torch.Tensor, w_vocab: torch.Tensor, ids: torch.Tensor, va
                    torch.empty((V, r), dtype=bf16, device=dev) if want_grads else None)
         loss, lse, d_rho, d_w = out
         teacher = _teacher(ids, values, rows, temperature, renormalise, dev)
-        ws = _scratch(workspace, head_distill_workspace_size(rows, V, r, teacher.k, d_rho is not None or d_w is not None), dev)
-        _check(lib().dls_head_distill(
+        grads = int(d_rho is not None or d_w is not None)
+        ws, size = _scratch(workspace, L.dls_head_distill_workspace_size(rows, V, r, teacher.k, grads), dev)
+        status = L.dls_head_distill(
             _vector(rho, "rho", (rows, r), bf16, dev), _vector(w_vocab, "w_vocab", (V, r), bf16, dev), rows, V, r, teacher,
             _vector(grad_loss, "grad_loss", (rows,), f32, dev), _vector(loss, "loss", (rows,), f32, dev),
             _vector(lse, "lse", (rows,), f32, dev), _vector(d_rho, "d_rho", (rows, r), bf16, dev),
-            _vector(d_w, "d_w", (V, r), bf16, dev), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+            _vector(d_w, "d_w", (V, r), bf16, dev), _address(ws), size, _stream_of(stream, dev))
+    _check(status)
     return loss, lse, d_rho, d_w
 
 

@@ -344,13 +344,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
     }, o.k, list, sh, put);
 }
 
-// With alternatives wanted, a merge reads parts x k keys, at most about 2,048 of them, and a part has at most kBlocks
-// blocks of four chunks a lane
+// With alternatives wanted, a part has at least 256 k entries (so that the k best blocks are few of its blocks), and at
+// most kBlocks blocks of four chunks a lane
 int logprobs_parts(int64_t rows, int32_t V, int elem_bytes, int k) {
   const int p = row_parts(rows, V, elem_bytes);
   if (k == 0) return p;
   const int most = kBlocks * kBlockLanes * 4 * (16 / elem_bytes);
-  return std::max(std::max(1, std::min(p, 2048 / k)), (V + most - 1) / most);
+  return std::max(std::max(1, std::min(p, V / (256 * k))), (V + most - 1) / most);
 }
 
 template <typename T>

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__
   });
   row_chunks<U>(
       row, g,
-      [&](const uint4* raw, auto n) {
+      [&](const uint4* raw, auto n, int) {
         float x[N * n];
 #pragma unroll
         for (int u = 0; u < n; ++u) Chunk<T>::widen(raw[u], x + u * N);

@@ -205,8 +205,8 @@ __device__ __forceinline__ float max_of(const float* x) {
 
 // Every chunk of the range, in iterations of U chunks a thread: eight lanes have the 8 U chunks of one block, 128 bytes
 // of it at a load, so that a block is one stretch of memory and the blocks, numbered iteration by iteration, rise
-// along the row.  `fold(raw, n)` gets n chunks at a time, U in every whole iteration, single ones in the last;
-// `pass(iteration)` comes after each.  Loads run an iteration ahead (chunks past the range clamped to its last: loaded,
+// along the row.  `fold(raw, n, u)` gets n chunks at a time, the iteration's u-th first: U in every whole iteration,
+// single ones in the last; `pass(iteration)` comes after each.  Loads run an iteration ahead (chunks past the range clamped to its last: loaded,
 // never folded).
 constexpr int kBlockLanes = 8;
 template <int U, typename T, typename Fold, typename Pass>
@@ -227,11 +227,11 @@ __device__ __forceinline__ void row_chunks(const T* row, const RowRange& r, Fold
 #pragma unroll
     for (int u = 0; u < U; ++u) next[u] = stream_load16(base + min(off + u * kBlockLanes * 16, last));
     if (b + NT * U <= r.c1) {
-      fold(raw, std::integral_constant<int, U>{});
+      fold(raw, std::integral_constant<int, U>{}, 0);
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (mine + (b - r.c0) + u * kBlockLanes < r.c1) fold(raw + u, std::integral_constant<int, 1>{});
+        if (mine + (b - r.c0) + u * kBlockLanes < r.c1) fold(raw + u, std::integral_constant<int, 1>{}, u);
     }
     pass(it);
 #pragma unroll

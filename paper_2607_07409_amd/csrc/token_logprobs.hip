@@ -1,7 +1,8 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits.
 //
 // One pass (row_stream.hpp) gives the log-sum-exp and the entropy.  The alternatives come out of the same pass: eight
-// lanes' chunks of an iteration are one stretch of the row, a block, and of each block the pass keeps the largest entry.
+// lanes' chunks of an iteration are one stretch of the row, a block (in short parts eight lanes' chunks of one load, so
+// that there are many more blocks than k), and of each block the pass keeps the largest entry.
 // Ordered by (value, lower block first), the k-th of these block maxima bounds the row's k best entries from below: k
 // blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.  Only the k
 // best blocks are read again (512 bytes each, from the caches), their entries at or above the bound are collected in
@@ -190,7 +191,7 @@ __device__ __forceinline__ void put_best(const RowOut& o, int64_t r, const RowSu
   o.logprobs[at] = key ? log_p(o, a, value_of(key), fast_log2(a.s)) : -INFINITY;
 }
 
-template <typename T, bool TOP, int U>
+template <typename T, bool TOP, int U, bool FINE>
 __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict__ L, int V, int64_t stride, RowOut o,
                                                             float4* __restrict__ part_sums,
                                                             u64* __restrict__ part_keys) {
@@ -204,17 +205,20 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   const int64_t r = blockIdx.x;
   const T* row = L + (size_t)r * stride;
   const RowRange g = row_range(row, V, part, parts);
-  const int nblocks = (g.c1 - g.c0 + NT * U - 1) / (NT * U) * (NT / kBlockLanes);   // <= kBlocks
+  constexpr int kSub = FINE ? U : 1, kBlockChunks = kBlockLanes * U / kSub, kPerIter = NT / kBlockLanes * kSub;
+  const int nblocks = (g.c1 - g.c0 + NT * U - 1) / (NT * U) * kPerIter;   // <= kBlocks
 
   RowSum a = row_empty();
-  float bm = -INFINITY;   // the largest of this thread's chunks of an iteration
+  float bm[kSub];   // the largest of this thread's chunks of an iteration
+#pragma unroll
+  for (int i = 0; i < kSub; ++i) bm[i] = -INFINITY;
   row_edges(g, V, part, parts, [&](int v) {
     const float x = to_f32(row[v]);
     row_fold<1, true>(a, &x, x, o.c);
   });
   row_chunks<U>(
       row, g,
-      [&](const uint4* raw, auto n) {
+      [&](const uint4* raw, auto n, int u0) {
         // masked entries of bf16 rows raised: the plain case of row_fold, without its test; otherwise as they are
         constexpr bool kRaise = sizeof(T) == 2;
         float x[N * n];
@@ -222,8 +226,18 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
         for (int u = 0; u < n; ++u) {
           Chunk<T>::widen(kRaise ? raise_masked(raw[u]) : raw[u], x + u * N);
         }
-        const float cm = max_of<N * n>(x);
-        if (TOP) bm = max3(bm, cm, cm);
+        float cm;
+        if (TOP && FINE) {
+          cm = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < n; ++u) {
+            bm[(u0 + u) % kSub] = max_of<N>(x + u * N);
+            cm = max3(cm, bm[(u0 + u) % kSub], cm);
+          }
+        } else {
+          cm = max_of<N * n>(x);
+          bm[0] = max3(bm[0], cm, cm);
+        }
         const bool move = cm * o.c > a.R + kLazy || a.R < -kPlainRef;
         if (__builtin_amdgcn_ballot_w64(move) && move) {
 #pragma unroll
@@ -235,10 +249,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
       },
       [&](int it) {
         if (!TOP) return;
-        const float m = lanes_max<kBlockLanes>(bm);
-        const int blk = it * (NT / kBlockLanes) + t / kBlockLanes;
-        if (t % kBlockLanes == 0) blocks[blk] = key_of(m, blk);
-        bm = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) {
+          const float m = lanes_max<kBlockLanes>(bm[i]);
+          const int blk = it * kPerIter + t / kBlockLanes * kSub + i;
+          if (t % kBlockLanes == 0) blocks[blk] = key_of(m, blk);
+          bm[i] = -INFINITY;
+        }
       });
   a = row_block_merge<true>(a, shr);
   if (t == 0) {
@@ -279,8 +296,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   // their entries, and the row's edge entries, as keys
   auto entries = [&](auto f) {
     row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
-    for (int w = t; w < nb * (kBlockLanes * U); w += NT) {
-      const int blk = chosen[w / (kBlockLanes * U)], c = g.c0 + blk * (kBlockLanes * U) + w % (kBlockLanes * U);
+    for (int w = t; w < nb * kBlockChunks; w += NT) {
+      const int blk = chosen[w / kBlockChunks], c = g.c0 + blk * kBlockChunks + w % kBlockChunks;
       if (c >= g.c1) continue;
       float x[N];
       Chunk<T>::load(row + g.h0 + (size_t)c * N, x);
@@ -362,10 +379,13 @@ hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
   float4* sums = (float4*)a.ws;
   u64* keys = (u64*)(a.ws + l.off_keys);
   const T* L = (const T*)a.logits;
-  // Long parts: few workgroups a CU, so four loads a thread in flight instead of two
+  // Long parts: few workgroups a CU, so four loads a thread in flight instead of two.  Fine blocks where they fit.
+  const int64_t chunks = (a.V / Chunk<T>::N + parts - 1) / parts;
   const bool four = a.V / parts > 16384;
-  const auto part = a.k > 0 ? (four ? k_logprobs_part<T, true, 4> : k_logprobs_part<T, true, 2>)
-                            : (four ? k_logprobs_part<T, false, 4> : k_logprobs_part<T, false, 2>);
+  const bool fine = (chunks + 1023) / 1024 * 1024 <= kBlocks * kBlockLanes;
+  const auto part = a.k == 0 ? (four ? k_logprobs_part<T, false, 4, false> : k_logprobs_part<T, false, 2, false>)
+                    : four   ? (fine ? k_logprobs_part<T, true, 4, true> : k_logprobs_part<T, true, 4, false>)
+                             : k_logprobs_part<T, true, 2, true>;
   part<<<grid, kThreads, 0, st>>>(L, a.V, a.stride, o, sums, keys);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;

@@ -143,12 +143,13 @@ __device__ __forceinline__ void hold_load(bf16x8 (&xf)[2][D / 16], const bf16_t*
 
 // The first product's matrix instructions are written out: their results belong in ordinary registers, where the
 // exponentials read them, while the accumulator registers hold nothing but the second product's sums (for r = 256 all
-// 256 of them).  results_settle: the distance that such a result must keep to the instructions that read it.
+// 256 of them).  The s_nop is the distance of an operand that the vector unit has just written; results_settle the one
+// that a result must keep to the instructions that read it.
 __device__ __forceinline__ void mfma_first(f32x16& d, bf16x8 a, bf16x8 b) {
-  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
+  asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_add(f32x16& d, bf16x8 a, bf16x8 b) {
-  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+  asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void results_settle(f32x16 (&s)[2]) {
   asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[0]), "+v"(s[1]));
@@ -404,12 +405,27 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
 // ------------------------------------------------------------------------------------------
 // a row's results
 // ------------------------------------------------------------------------------------------
+// A tile's rows: R + log2 s - log2 |g M / T|, so that 2^(y - l) is the entry's weight of the row, and the weight's sign in
+// the place of a bf16's.  64 words, one a lane's.
+struct RowTile {
+  float l[kTile];
+  uint16_t sign[kTile];
+  uint32_t unused[kTile / 2];
+};
+static_assert(sizeof(RowTile) == 256, "a word a lane");
+
 struct HeadOut {
   float *loss, *lse;       // either may be NULL
   bf16_t* d_rho;           // with gradients: [rows, r]
-  float2* row;             //   (R + log2 s, g M / T) in the order of k_head_w's tiles
+  float* row;              //   what k_head_w needs of each row, by tiles (RowTile)
   float* coef;             //   [rows, K]: -g q_k / T of each entry
 };
+
+__device__ __forceinline__ void put_row(float* rows, int64_t place, float l, bool negative) {
+  RowTile* t = reinterpret_cast<RowTile*>(rows) + place / kTile;
+  t->l[place % kTile] = l;
+  t->sign[place % kTile] = negative ? 0x8000 : 0;
+}
 
 __device__ __forceinline__ float4 widen4(uint2 v) {
   return make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
@@ -501,13 +517,14 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
     if (o.lse) o.lse[row] = row_lse(a);
     if (GRAD) {   // the last of several tiles ends with the last row
       const int64_t whole = rows / kTile * kTile, pad = rows > kTile && rows > whole ? whole + kTile - rows : 0;
-      o.row[row < whole ? row : row + pad] = make_float2(a.R + l2, w * mass);
+      const float f = w * mass;
+      put_row(o.row, row < whole ? row : row + pad, f != 0.f ? a.R + l2 - fast_log2(fabsf(f)) : kMostY, f < 0.f);
     }
   }
   if (GRAD) {
-    // the places of its tile that no row has: 2^-kMostY times 0
+    // the places of its tile that no row has: 2^-kMostY = 0
     const int64_t whole = rows / kTile * kTile, left = rows - whole;
-    if (row == rows - 1 && left > 0 && t < kTile - left) o.row[rows > kTile ? whole + t : rows + t] = make_float2(kMostY, 0.f);
+    if (row == rows - 1 && left > 0 && t < kTile - left) put_row(o.row, rows > kTile ? whole + t : rows + t, kMostY, false);
     if (t < te.k) o.coef[(size_t)row * te.k + t] = -w * e.q;
     if (wave == 0 && on) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -686,7 +703,7 @@ __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)"
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                         int64_t rows, int V, int r, float c,
-                                                        const float2* __restrict__ row_stats,
+                                                        const RowTile* __restrict__ row_tiles,
                                                         const uint32_t* __restrict__ begin,
                                                         const uint2* __restrict__ list, int whole, int splits,
                                                         bf16_t* __restrict__ d_w, float* __restrict__ part_w) {
@@ -697,7 +714,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   // the stream's buffers; after it a tile of each wave
   static_assert(kBuffers >= kWaves, "the stream's buffers hold the waves' own tiles");
   __shared__ Tile<D> tiles[kBuffers];
-  __shared__ float2 stats[kBuffers][kWaves][kTile];   // of a tile's rows, a copy for each wave
+  __shared__ RowTile stats[kBuffers][kWaves];         // a copy for each wave
   __shared__ float wide[kWaves][kTile * kHeadGroup];  // a tile's coefficients of the teacher's entries
   __shared__ int range[2][kWaves];
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, t = threadIdx.x;
@@ -707,7 +724,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   const int t0 = (int)((int64_t)all * part / parts), nt = (int)((int64_t)all * (part + 1) / parts);
   const TileStream<D> rho_tiles(rho, rows, r);
   auto stream = [&](int tile, int to) {
-    stream_to_lds4(row_stats + (size_t)tile * kTile, 4 * lane, lds_address(stats[to][wave]));
+    stream_to_lds4(row_tiles + tile, 4 * lane, lds_address(&stats[to][wave]));
     rho_tiles.start(tiles[to], tile);
   };
 
@@ -723,18 +740,17 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   int at = 0, before = 0;
   for (int k = t0; k < nt; ++k) {
     const int next = next_buffer(at), free = next_buffer(next_buffer(next));
-    const float2* st = stats[at][wave];
+    const RowTile& st = stats[at][wave];
     f32x16 s[2];
     product_s<D>(s, a, tiles[at], xf);
     stream_wait<kLoads>();
     __syncthreads();
     Exponentials<D> ex;
     Words now;
-    auto stat = [&](int i) { return st[8 * (i >> 2) + 4 * h + (i & 3)]; };
-    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -stat(i).x)); };
+    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -st.l[8 * (i >> 2) + 4 * h + (i & 3)])); };
     auto end = [&](int x, int i, float e) {
-      e *= stat(i).y;
-      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], e);
+      if (i % 2)
+        now.w[x][i / 2] = pack2(ex.e[x][i - 1], e) ^ *reinterpret_cast<const uint32_t*>(st.sign + 8 * (i >> 2) + 4 * h + (i & 2));
       return e;
     };
     product_o<D>(o, tiles[before], p, [&](int q) {
@@ -779,6 +795,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
   }
   while (many ? k < last : b < b1) {
     const uint32_t from = b;
+    uint32_t batch = b;   // where en, and then old, begins
+    uint2 old[4];
     int first = 0;
     if (many) {
       stream_wait<2 * Tile<D>::kLoads>();   // (the loads of entries only make it wait for more)
@@ -795,10 +813,16 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
           if (in) unsafeAtomicAdd(q + (row - first) * kHeadGroup + (en[u].x >> 24), __uint_as_float(en[u].y));
           found += __popcll(__builtin_amdgcn_ballot_w64(in));
         }
+        batch = b;
         b += found;
         if (found < 256 || b >= b1) break;
 #pragma unroll
         for (int u = 0; u < 4; ++u) en[u] = list[min(b + u * 64 + lane, end)];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        old[u] = en[u];
+        en[u] = list[min(b + u * 64 + lane, end)];   // (the next tile's, on their way beside the products)
       }
       ++k;
     } else {
@@ -814,12 +838,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
       lds_done();
       coefficient_products<D>(o, tiles[many ? at : wave], q);
       if (many) {
-        for (uint32_t i = from + lane; i < b; i += 64) {
+        for (uint32_t i = from + lane; i < batch; i += 64) {   // (more than 256 of a tile)
           const uint32_t x = list[i].x;
           q[((x & 0xffffffu) - first) * kHeadGroup + (x >> 24)] = 0.f;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) en[u] = list[min(b + u * 64 + lane, end)];
+        for (int u = 0; u < 4; ++u)
+          if (batch + u * 64 + lane < b) q[((old[u].x & 0xffffffu) - first) * kHeadGroup + (old[u].x >> 24)] = 0.f;
       } else if (h == 0) {
         q[n * kHeadGroup + (en[1].x >> 24)] = 0.f;
       }
@@ -891,7 +916,7 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   o.d_rho = (bf16_t*)a.d_rho;
-  o.row = (float2*)(a.ws + l.off_row);
+  o.row = (float*)(a.ws + l.off_row);
   o.coef = (float*)(a.ws + l.off_coef);
   uint32_t *counts = (uint32_t*)(a.ws + l.off_counts), *totals = (uint32_t*)(a.ws + l.off_totals);
   uint32_t* begin = totals + l.keys;
@@ -912,7 +937,7 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   float* part_w = (float*)(a.ws + l.off_o);   // (the splits' sums are joined by now)
   k_head_w<D><<<(unsigned)(l.whole + (l.tiles - l.whole) * l.row_splits), kThreads, 0, st>>>(
-      rho, W, a.rows, a.V, a.r, a.teacher.c, o.row, begin, list, l.whole, l.row_splits, (bf16_t*)a.d_w, part_w);
+      rho, W, a.rows, a.V, a.r, a.teacher.c, (const RowTile*)o.row, begin, list, l.whole, l.row_splits, (bf16_t*)a.d_w, part_w);
   if ((e = hipGetLastError()) != hipSuccess || l.whole == l.tiles) return e;
   const int64_t elems = (int64_t)(l.tiles - l.whole) * kHold * a.r;
   k_head_join<<<(unsigned)((elems / 8 + kThreads - 1) / kThreads), kThreads, 0, st>>>(part_w, l.row_splits, (int64_t)l.whole * kHold,
@@ -941,7 +966,7 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
     l.off_o = at;
     at += up(std::max((size_t)l.splits * rows, (size_t)(l.tiles - l.whole) * l.row_splits * kHold) * r * sizeof(float));
     l.off_row = at;
-    at += up((size_t)(rows + kTile) * sizeof(float2));
+    at += up((size_t)((rows + kTile - 1) / kTile) * sizeof(RowTile));
     l.off_coef = at;
     at += up((size_t)n * sizeof(float));
     l.off_counts = at;

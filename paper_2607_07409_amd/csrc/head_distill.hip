@@ -747,14 +747,27 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
     __syncthreads();
     Exponentials<D> ex;
     Words now;
-    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -st.l[8 * (i >> 2) + 4 * h + (i & 3)])); };
+    // four rows' numbers at a time, read while the four before are used (a read just before its use would be waited for,
+    // with all the reads of Y before it)
+    float4 l[4];
+    uint2 sign[4];
+    auto rows_of = [&](int g) {
+      l[g] = *reinterpret_cast<const float4*>(st.l + 8 * g + 4 * h);
+      sign[g] = *reinterpret_cast<const uint2*>(st.sign + 8 * g + 4 * h);
+    };
+    auto begin = [&](int x, int i) {
+      const float4 f = l[i >> 2];
+      return fast_exp2(__builtin_fmaf(s[x][i], c, -(i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w)));
+    };
     auto end = [&](int x, int i, float e) {
-      if (i % 2)
-        now.w[x][i / 2] = pack2(ex.e[x][i - 1], e) ^ *reinterpret_cast<const uint32_t*>(st.sign + 8 * (i >> 2) + 4 * h + (i & 2));
+      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], e) ^ (i % 4 == 1 ? sign[i >> 2].x : sign[i >> 2].y);
       return e;
     };
+    rows_of(0);
     product_o<D>(o, tiles[before], p, [&](int q) {
+      constexpr int kPer = Exponentials<D>::kPer;
       if (q == 0) stream(min(k + 3, nt - 1), free);
+      if (q * kPer % 4 == 0 && q * kPer / 4 < 3) rows_of(q * kPer / 4 + 1);
       ex.step(q, begin, end);
     });
     pieces_first(a, tiles[next]);

@@ -546,10 +546,27 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
 // ------------------------------------------------------------------------------------------
 extern __shared__ uint32_t key_lds[];   // a word per key
 
-__device__ __forceinline__ int entry_key(const TeacherArgs& te, int64_t e, int64_t n, int V) {
-  if (e >= n) return -1;
-  const int id = te.ids[e];
-  return id >= 0 && id < V && te.values[e] > -INFINITY ? id / kHeadGroup : -1;
+// A wave's entries are taken 512 at a time, eight a lane, whose loads are all in flight together.
+constexpr int kSortLoads = 8;
+struct SortEntry {
+  int id;        // -1: absent
+  float coef;
+};
+// entries e0 + 64 u + lane below `end`
+template <bool COEF>
+__device__ __forceinline__ void sort_load(SortEntry (&en)[kSortLoads], const TeacherArgs& te, const float* coef,
+                                          int64_t e0, int64_t end, int V) {
+  float y[kSortLoads];
+#pragma unroll
+  for (int u = 0; u < kSortLoads; ++u) {
+    const int64_t e = e0 + u * 64 + (threadIdx.x & 63);
+    en[u].id = e < end ? te.ids[e] : -1;
+    y[u] = e < end ? te.values[e] : -INFINITY;
+    if (COEF) en[u].coef = e < end ? coef[e] : 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < kSortLoads; ++u)
+    if (en[u].id < 0 || en[u].id >= V || !(y[u] > -INFINITY)) en[u].id = -1;
 }
 
 // one wave per chunk of the entries: how many of each key
@@ -558,10 +575,13 @@ __global__ __launch_bounds__(64) void k_sort_count(TeacherArgs te, int64_t n, in
   const int lane = threadIdx.x;
   for (int i = lane; i < keys; i += 64) key_lds[i] = 0;
   __syncthreads();
-  const int64_t e0 = (int64_t)blockIdx.x * chunk;
-  for (int i = lane; i < chunk; i += 64) {
-    const int key = entry_key(te, e0 + i, n, V);
-    if (key >= 0) atomicAdd(&key_lds[key], 1u);
+  const int64_t e0 = (int64_t)blockIdx.x * chunk, end = min(e0 + chunk, n);
+  for (int64_t e = e0; e < end; e += 64 * kSortLoads) {
+    SortEntry en[kSortLoads];
+    sort_load<false>(en, te, nullptr, e, end, V);
+#pragma unroll
+    for (int u = 0; u < kSortLoads; ++u)
+      if (en[u].id >= 0) atomicAdd(&key_lds[en[u].id / kHeadGroup], 1u);
   }
   __syncthreads();
   for (int i = lane; i < keys; i += 64) counts[(size_t)blockIdx.x * keys + i] = key_lds[i];
@@ -628,26 +648,30 @@ __global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, in
   const int lane = threadIdx.x;
   for (int i = lane; i < keys; i += 64) key_lds[i] = begin[i] + counts[(size_t)blockIdx.x * keys + i];
   __syncthreads();
-  const int64_t e0 = (int64_t)blockIdx.x * chunk;
-  for (int i = 0; i < chunk; i += 64) {
-    const int64_t e = e0 + i + lane;
-    const int key = entry_key(te, e, n, V);
-    uint64_t same = __builtin_amdgcn_ballot_w64(key >= 0);   // lanes of the same key
-    if (!same) continue;
+  const int64_t e0 = (int64_t)blockIdx.x * chunk, end = min(e0 + chunk, n);
+  for (int64_t e = e0; e < end; e += 64 * kSortLoads) {
+    SortEntry en[kSortLoads];
+    sort_load<true>(en, te, coef, e, end, V);
 #pragma unroll
-    for (int b = 0; (1 << b) < kHeadMostKeys; ++b) {
-      const bool bit = (key >> b) & 1;
-      const uint64_t set = __builtin_amdgcn_ballot_w64(bit);
-      same &= bit ? set : ~set;
+    for (int u = 0; u < kSortLoads; ++u) {
+      const int key = en[u].id < 0 ? -1 : en[u].id / kHeadGroup;
+      uint64_t same = __builtin_amdgcn_ballot_w64(key >= 0);   // lanes of the same key
+      if (!same) continue;
+#pragma unroll
+      for (int b = 0; (1 << b) < kHeadMostKeys; ++b) {
+        const bool bit = (key >> b) & 1;
+        const uint64_t set = __builtin_amdgcn_ballot_w64(bit);
+        same &= bit ? set : ~set;
+      }
+      if (key >= 0) {
+        const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+        list[key_lds[key] + rank] = make_uint2((uint32_t)((e + u * 64 + lane) / te.k) | (uint32_t)(en[u].id % kHeadGroup) << 24,
+                                               __float_as_uint(en[u].coef));
+      }
+      __syncthreads();
+      if (key >= 0 && (same >> lane) == 1) key_lds[key] += __popcll(same);   // the last lane of the key
+      __syncthreads();
     }
-    if (key >= 0) {
-      const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-      list[key_lds[key] + rank] =
-          make_uint2((uint32_t)(e / te.k) | (uint32_t)(te.ids[e] % kHeadGroup) << 24, __float_as_uint(coef[e]));
-    }
-    __syncthreads();
-    if (key >= 0 && (same >> lane) == 1) key_lds[key] += __popcll(same);   // the last lane of the key
-    __syncthreads();
   }
 }
 

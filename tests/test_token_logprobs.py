@@ -278,5 +278,6 @@ def test_entry_point_takes_no_rows_and_sizes():
     assert _call(rows=0, logits=None, stats=None) == 0
     assert B.token_logprobs_workspace_size(0, 1000, 5) == 0 and B.token_logprobs_workspace_size(4, 1000, 999) == 0
     assert B.token_logprobs_workspace_size(1, 151936, 5) > 0
-    # rows past the split hold no parts
-    assert B.token_logprobs_workspace_size(1024, 151936, 5) == 0
+    # rows past the split hold no parts, where one workgroup can hold the block maxima of a row of either type
+    assert B.token_logprobs_workspace_size(1024, 100003, 5) == 0
+    assert B.token_logprobs_workspace_size(1024, 151936, 5) > 0

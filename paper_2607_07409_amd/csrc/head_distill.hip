@@ -7,16 +7,26 @@
 //   k_head_rho  holds 64 rows of rho a wave and streams W: running sum of exponentials and sum_v 2^(y_v - R) W_v
 //   k_head_w    holds 64 rows of W a wave and streams rho: p is known by then, d_W is summed over all rows
 // so the gradients cost four products of rows x V x r instead of three and no row of logits touches memory.  The
-// streamed operand Y passes through LDS in tiles of 32 rows, 16-byte pieces swizzled by row.  The first product is
+// streamed operand Y passes through LDS in tiles of 32 rows (Tile).  The first product is
 // S^T = Y X^T (v_mfma_f32_32x32x16_bf16, products exact, sums float32): its result has the held row X in the lane and
 // the streamed rows in registers, which is what the second product wants as its left operand, X x d = P^T Y, after
 // rounding to bf16; the right operand is the same LDS tile read transposed.  Only that rounding of the
-// probabilities (2^-9 relative, each on its own) is below float32, as the gradients' own type is.
+// probabilities (2^-8 relative, each on its own) is below float32, as the gradients' own type is.
 //
 // The teacher's entries: k_head_finish (one workgroup per row) takes their logits and their part of d_rho from W's
 // rows directly, in float32.  Their part of d_W is summed in k_head_w: the entries are put in order of the vocabulary
 // tile by a stable counting sort (so the sum's order, and every bit, is the same in every run) and streamed after the
 // rows as further tiles of Y, with their coefficients as two bf16 terms.
+//
+// Why 64 rows held a wave: every tile of Y read from LDS then meets two tiles of X, which halves the LDS reads for each
+// product, and at r = 256 the second product's sums are just the 256 accumulator registers that a lane has.  That is one
+// wave a SIMD, so nothing but the wave itself hides its latencies: the streams run three tiles ahead, and the
+// exponentials of a tile stand between the matrix instructions of the tile before.
+//
+// Measured at 6,001 rows, V = 151,936, r = 256, K = 50: 1,644 us a call, of which k_head_rho 795 and k_head_w 876 in a
+// profile (two products of 467 GFLOP each: 1.17 and 1.07 PFLOP/s; a library product of 8192^3 reaches 1.20 to 1.52),
+// k_head_finish 38, the sort 50 to 65.  At 1,024 rows 416 us; 96 rows of V = 32,003, r = 128: 68 us, of which seven
+// launches and their ramps are most.  The loss alone of 256 rows: 37 to 39 us, W read once in 12.
 #include "teacher.hpp"
 
 namespace dls {
@@ -929,9 +939,10 @@ __global__ __launch_bounds__(kThreads) void k_zero(uint4* __restrict__ p, int64_
 // Workgroups at a time: one per CU, a wave of rank 256 or 128 with gradients holding its SIMD's registers, else two
 constexpr int kSlots = 256;
 int head_splits(int64_t rows, int V, bool grads) {
-  // of the vocabulary, where rho is held: a slot each; every split at least 8 tiles
+  // of the vocabulary, where rho is held: a slot each; every split at least 4 tiles (46 rows at V = 9,176: 73 us a call,
+  // with at least 8 tiles 76)
   const int64_t blocks = (rows + kHold - 1) / kHold;
-  const int64_t cap = std::max<int64_t>(1, V / (8 * kTile)), slots = grads ? kSlots : 2 * kSlots;
+  const int64_t cap = std::max<int64_t>(1, V / (4 * kTile)), slots = grads ? kSlots : 2 * kSlots;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / std::max<int64_t>(1, blocks), cap), kHeadMostSplits));
 }
 
@@ -990,9 +1001,10 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
   l.splits = head_splits(rows, V, grads);
   l.tiles = (V + kHold - 1) / kHold;
   l.keys = l.tiles * (kHold / kHeadGroup);   // every wave's, also past V
-  // the tiles that the last round of workgroups has too few of share a slot's rows: parts of at least 8 tiles of rows
+  // the tiles that the last round of workgroups has too few of share a slot's rows: parts of at least 4 tiles of rows
+  // (483 rows at V = 10,911: 110 us a call, with at least 8 tiles 138; 1,500 rows at V = 32,003: 228 either way)
   const int left = l.tiles % kSlots;
-  l.row_splits = left ? (int)std::max<int64_t>(1, std::min<int64_t>(kSlots / left, rows / (8 * kTile))) : 1;
+  l.row_splits = left ? (int)std::max<int64_t>(1, std::min<int64_t>(kSlots / left, rows / (4 * kTile))) : 1;
   l.whole = l.row_splits > 1 ? l.tiles - left : l.tiles;
   const int64_t n = rows * k;
   // chunks of at least 512 entries, at most 1,024 of them

@@ -3,8 +3,9 @@
 The teacher's rows of logits give, through token_logprobs, the K most likely tokens of every position with their log
 probabilities: all that is kept of it.  The student's logits are rho W^T, with fixed low-rank states rho (in a local head
 SiLU(W_rank h)); head_distill computes the loss and the gradient by W without storing them, and Adam keeps a float32 copy of
-W.  (The K entries are not all of the teacher, so the loss, a part of a divergence, may fall below 0.)  At the end it is computed once more from stored logits (distill_loss), and the log probability that the student
-gives the teacher's first choice is compared with what it was.
+W.  (The K entries are not all of the teacher, so the loss, a part of a divergence, may fall below 0.)  At the end it is
+computed once more from stored logits (distill_loss), and the log probability that the student gives the teacher's first
+choice is compared with what it was.
 
     python examples/distill_head.py [--rows 1024] [--vocab 32003] [--rank 128] [--top-k 32] [--steps 60]
 """

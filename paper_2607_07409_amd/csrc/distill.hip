@@ -5,6 +5,10 @@
 // The loss needs the row's log-sum-exp, one pass over the logits (row_stream.hpp), and K entries.  The gradient is a
 // second pass that reads an entry and writes one; the teacher's entries of a workgroup's range are written after it,
 // each from its own logit in float32 and rounded once (several entries of one id by the first of them).
+//
+// What bounds it: reads and writes.  2,048 bf16 rows of V = 151,936, loss and gradient in 243 to 254 us: 4.9 to 5.1 TB/s
+// of the 1.24 GB read and written, where a large copy reaches 4.93.  The gradient alone of 777 rows of V = 70,001 in
+// 55.7 us (3.9 TB/s).  Small calls are latency: 16 rows of V = 32,003, loss and gradient, 8.9 us of kernel.
 #include "teacher.hpp"
 
 namespace dls {
@@ -34,7 +38,7 @@ __device__ __forceinline__ void finish_row(const T* row, int V, int64_t r, const
   }
 }
 
-template <typename T, int U>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__ L, int V, int64_t stride, TeacherArgs te,
                                                            float2* __restrict__ part_sums, LossOut o) {
   constexpr int N = Chunk<T>::N;
@@ -49,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_part(const T* __restrict__
     const float x = to_f32(row[v]);
     row_fold<1, false>(a, &x, x, te.c);
   });
-  row_chunks<U>(
+  row_chunks<2>(   // (four loads a thread in flight are slower: 2,048 rows of V = 32,003 in 31.0 us, with two 28.6)
       row, g,
       [&](const uint4* raw, auto n, int) {
         float x[N * n];
@@ -303,7 +307,10 @@ hipError_t launch_grad_t(const DistillArgs& a, const float2* row_stats, hipStrea
   return hipGetLastError();
 }
 
-// A row whose pieces fit a workgroup's registers is read once
+// A row whose pieces fit a workgroup's registers is read once, else twice, by the loss's kernels and k_distill_grad (700
+// rows of V = 32,003: 25 us and 37; 2,048 of V = 151,936: 254 and 376).  By 1,024 threads, the least work for each; from
+// 512 rows on (two a CU) short ones by 256, so that several rows are in flight on a CU (V = 32,003, 700 rows: 25.2 us,
+// with 1,024 threads 27.8; 300 rows: 20.4 and 17.2).
 template <typename T, int NT, int NCH>
 hipError_t launch_row_t(const DistillArgs& a, hipStream_t st) {
   const LossOut o = {a.out_loss, a.out_lse, nullptr};
@@ -317,7 +324,6 @@ template <typename T>
 hipError_t launch_row(const DistillArgs& a, hipStream_t st) {
   const int64_t pieces = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
   if (a.rows >= 512 && pieces <= 256 * 20) return launch_row_t<T, 256, 20>(a, st);
-  if (a.rows >= 512 && pieces <= 512 * 20) return launch_row_t<T, 512, 20>(a, st);
   return pieces <= 1024 * 5    ? launch_row_t<T, 1024, 5>(a, st)
          : pieces <= 1024 * 10 ? launch_row_t<T, 1024, 10>(a, st)
                                : launch_row_t<T, 1024, 20>(a, st);
@@ -331,9 +337,7 @@ hipError_t launch_loss_t(const DistillArgs& a, hipStream_t st) {
   float2* sums = rows + a.rows;
   const LossOut o = {a.out_loss, a.out_lse, a.grad ? rows : nullptr};
   const T* L = (const T*)a.logits;
-  // whole rows: few workgroups a CU, so four loads a thread in flight instead of two
-  const auto part = parts == 1 ? k_distill_part<T, 4> : k_distill_part<T, 2>;
-  part<<<dim3((unsigned)a.rows, (unsigned)parts), kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, sums, o);
+  k_distill_part<T><<<dim3((unsigned)a.rows, (unsigned)parts), kThreads, 0, st>>>(L, a.V, a.stride, a.teacher, sums, o);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (parts > 1) {

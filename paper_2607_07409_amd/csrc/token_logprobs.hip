@@ -13,6 +13,10 @@
 // Keys: a value's bits as an integer of the same order in the upper half, the complement of the index (or block) in
 // the lower, so that the larger key is the better entry, ties going to the lower index, and no two are equal.  0 is
 // no key.  Masked entries (-inf) and NaN have none.
+//
+// What bounds it: many rows, the read (1,024 bf16 rows of V = 151,936 with their 20 best: 64 us a call; only reading
+// them takes 55, and 46 at the 6.75 TB/s that one large array is read with).  Few rows, the chain of launch, a part's
+// pass, its selection and the merge (16 such rows: 10.4 us the parts, 4.7 the merge; a row with its 5 best: 6.7 and 3.4).
 #include "row_stream.hpp"
 
 namespace dls {
@@ -362,7 +366,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_merge(const T* __restrict
 }
 
 // With alternatives wanted, a part has at least 256 k entries (so that the k best blocks are few of its blocks), and at
-// most kBlocks blocks of four chunks a lane
+// most kBlocks blocks of four chunks a lane.  (300 float32 rows of V = 32,003, the 64 best: 22.1 us a call; with at least
+// 128 k entries 26.4, with 64 k 27.8.)
 int logprobs_parts(int64_t rows, int32_t V, int elem_bytes, int k) {
   const int p = row_parts(rows, V, elem_bytes);
   if (k == 0) return p;
@@ -379,7 +384,9 @@ hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
   float4* sums = (float4*)a.ws;
   u64* keys = (u64*)(a.ws + l.off_keys);
   const T* L = (const T*)a.logits;
-  // Long parts: few workgroups a CU, so four loads a thread in flight instead of two.  Fine blocks where they fit.
+  // Long parts: four loads a thread in flight and, with alternatives, blocks of all four, so that they fit LDS.  Short
+  // ones: two (300 rows of V = 32,003: 17.5 us, with four 18.3).  Fine blocks where they fit (1,024 rows of V = 32,003:
+  // 24.2 us, else 25.0; 300 float32 rows with the 64 best: 21.9, else 24.2).
   const int64_t chunks = (a.V / Chunk<T>::N + parts - 1) / parts;
   const bool four = a.V / parts > 16384;
   const bool fine = (chunks + 1023) / 1024 * 1024 <= kBlocks * kBlockLanes;

@@ -309,8 +309,8 @@ hipError_t launch_grad_t(const DistillArgs& a, const float2* row_stats, hipStrea
 
 // A row whose pieces fit a workgroup's registers is read once, else twice, by the loss's kernels and k_distill_grad (700
 // rows of V = 32,003: 25 us and 37; 2,048 of V = 151,936: 254 and 376).  By 1,024 threads, the least work for each; from
-// 512 rows on (two a CU) short ones by 256, so that several rows are in flight on a CU (V = 32,003, 700 rows: 25.2 us,
-// with 1,024 threads 27.8; 300 rows: 20.4 and 17.2).
+// 512 rows on (two a CU) short ones by 256, so that several rows are in flight on a CU (V = 16,001: 1,100 rows in 22.7 us,
+// with 1,024 threads 34; 1,500 rows of V = 24,001 37 and 44).
 template <typename T, int NT, int NCH>
 hipError_t launch_row_t(const DistillArgs& a, hipStream_t st) {
   const LossOut o = {a.out_loss, a.out_lse, nullptr};
@@ -319,11 +319,16 @@ hipError_t launch_row_t(const DistillArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 template <typename T>
-bool row_fits(int32_t V) { return V <= 1024 * 20 * Chunk<T>::N; }
+bool row_fits(int64_t rows, int32_t V) {
+  // (few long rows: split over the card they are done sooner, also if read twice; 64 bf16 rows of V = 151,936 in 21.4 us,
+  // by a workgroup each 24.9; of V = 100,003 20.3 and 20.5, of 70,001 20.2 and 16.8; 128 of V = 151,936 28.4 and 25.6)
+  if (rows <= 64 && V > 100000) return false;
+  return V <= 1024 * 20 * Chunk<T>::N;
+}
 template <typename T>
 hipError_t launch_row(const DistillArgs& a, hipStream_t st) {
   const int64_t pieces = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
-  if (a.rows >= 512 && pieces <= 256 * 20) return launch_row_t<T, 256, 20>(a, st);
+  if (a.rows >= 512 && pieces <= 256 * 12) return launch_row_t<T, 256, 12>(a, st);
   return pieces <= 1024 * 5    ? launch_row_t<T, 1024, 5>(a, st)
          : pieces <= 1024 * 10 ? launch_row_t<T, 1024, 10>(a, st)
                                : launch_row_t<T, 1024, 20>(a, st);
@@ -331,7 +336,7 @@ hipError_t launch_row(const DistillArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_loss_t(const DistillArgs& a, hipStream_t st) {
-  if (a.grad && row_fits<T>(a.V)) return launch_row<T>(a, st);
+  if (a.grad && row_fits<T>(a.rows, a.V)) return launch_row<T>(a, st);
   const int parts = row_parts(a.rows, a.V, (int)sizeof(T));
   float2* rows = (float2*)a.ws;
   float2* sums = rows + a.rows;

@@ -160,6 +160,18 @@ def test_gradient_in_place(rows, V, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,V,dtype", [(64, 100003, BF16), (65, 100003, BF16), (64, 99999, BF16), (65, 81919, F32), (513, 24571, BF16), (513, 24577, BF16), (513, 12287, F32)])
+def test_where_the_choice_of_kernel_changes(rows, V, dtype):
+    """Numbers of rows and lengths at which another kernel or workgroup takes over, also with the gradient in place."""
+    x, (ids, y), w = _student(rows, V, dtype, 41, pad=1), _teacher(rows, V, 30, 42, ragged=True), _weight(rows, 43)
+    grad = _all(x, ids, y, w, 1.0, True, rows=[0, 1, rows // 2, rows - 1])[2]
+    s = torch.empty((rows, V + 1), dtype=dtype, device="cuda")[:, :V].copy_(x)
+    loss, lse, _ = B.distill_loss(s, ids, y, grad_loss=w, out=(torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), s))
+    _check(x, ids, y, w, 1.0, True, loss=loss, lse=lse, grad=s, rows=[0, 1, rows // 2, rows - 1])
+    assert torch.equal(s, grad)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("whole", [False, True])
 def test_special_rows(whole, dtype):

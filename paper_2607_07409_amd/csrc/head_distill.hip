@@ -23,9 +23,9 @@
 // wave a SIMD, so nothing but the wave itself hides its latencies: the streams run three tiles ahead, and the
 // exponentials of a tile stand between the matrix instructions of the tile before.
 //
-// Measured at 6,001 rows, V = 151,936, r = 256, K = 50: 1,644 us a call, of which k_head_rho 795 and k_head_w 876 in a
-// profile (two products of 467 GFLOP each: 1.17 and 1.07 PFLOP/s; a library product of 8192^3 reaches 1.20 to 1.52),
-// k_head_finish 38, the sort 50 to 65.  At 1,024 rows 416 us; 96 rows of V = 32,003, r = 128: 68 us, of which seven
+// Measured at 6,001 rows, V = 151,936, r = 256, K = 50: 1,644 to 1,706 us a call; in a profile k_head_rho 746 and k_head_w
+// 859 (two products of 467 GFLOP each: 1.25 and 1.09 PFLOP/s; a library product of 8192^3 reaches 1.20 to 1.52),
+// k_head_finish 36, the sort 54.  At 1,024 rows 416 us; 96 rows of V = 32,003, r = 128: 68 us, of which seven
 // launches and their ramps are most.  The loss alone of 256 rows: 37 to 39 us, W read once in 12.
 #include "teacher.hpp"
 

@@ -461,8 +461,8 @@ dls_status dls_distill_grad(const void *logits, dls_dtype dtype, int64_t rows, i
  *   workspace    at least dls_head_distill_workspace_size bytes, 256-byte aligned; its content does
  *                not matter (with gradients: rows r 4 bytes for each of up to 256 splits of the
  *                vocabulary, 8 bytes a teacher entry twice, and small)
- * Products are exact and summed in float32; within the gradients the probabilities are rounded to
- * bf16, as the results are.  Results do not depend on anything but the arguments (no atomic sums).
+ * Products are exact and summed in float32; within the gradients each g / T (M p_v - q_v), a difference of float32 numbers,
+ * counts to 2^-8 of itself, as the results do.  Results do not depend on anything but the arguments (no atomic sums).
  * Limits: 0 <= rows <= 2^20, 1 <= V <= 2^20, r a multiple of 8 with 8 <= r <= 256; finite rho and W. */
 size_t dls_head_distill_workspace_size(int64_t rows, int32_t V, int32_t r, int32_t k, int with_gradients);
 dls_status dls_head_distill(const void *rho, const void *w_vocab, int64_t rows, int32_t V, int32_t r,

@@ -143,7 +143,7 @@ struct HeadLayout {
   int tiles;                 // of the vocabulary, where W is held: `whole` by a workgroup each, the others by
   int whole, row_splits;     // row_splits workgroups
   int keys, chunk, chunks;   // of the counting sort of the teacher's entries
-  size_t off_o, off_row, off_coef, off_counts, off_totals, off_list, total;
+  size_t off_o, off_row, off_id, off_coef, off_counts, off_totals, off_list, total;
 };
 HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads);
 hipError_t launch_head_distill(const HeadDistillArgs& a, hipStream_t st);

@@ -10,13 +10,16 @@
 // streamed operand Y passes through LDS in tiles of 32 rows (Tile).  The first product is
 // S^T = Y X^T (v_mfma_f32_32x32x16_bf16, products exact, sums float32): its result has the held row X in the lane and
 // the streamed rows in registers, which is what the second product wants as its left operand, X x d = P^T Y, after
-// rounding to bf16; the right operand is the same LDS tile read transposed.  Only that rounding of the
-// probabilities (2^-8 relative, each on its own) is below float32, as the gradients' own type is.
+// rounding to bf16; the right operand is the same LDS tile read transposed.  That rounding (2^-9 relative, each
+// probability on its own) is below float32, as the gradients' own type is.  It may stand where a probability is all that
+// its token has in d; where q is taken from it, and p is near q once the student has learnt, it would be what is left.
 //
-// The teacher's entries: k_head_finish (one workgroup per row) takes their logits and their part of d_rho from W's
-// rows directly, in float32.  Their part of d_W is summed in k_head_w: the entries are put in order of the vocabulary
-// tile by a stable counting sort (so the sum's order, and every bit, is the same in every run) and streamed after the
-// rows as further tiles of Y, with their coefficients as two bf16 terms.
+// The teacher's entries: k_head_finish (one workgroup per row) computes their logits to the bits of the two kernels, so it
+// knows what each rounded, and gives an entry the coefficient -g q / T and the lost part of g / T M p: with the dense part
+// that makes g / T (M p - q) in float32.  Their part of d_rho is summed there, from W's rows.  Their part of d_W is summed
+// in k_head_w: the entries (several of one id as one) are put in order of the vocabulary tile by a stable counting sort (so
+// the sum's order, and every bit, is the same in every run) and streamed after the rows as further tiles of Y, with their
+// coefficients as two bf16 terms.
 //
 // Why 64 rows held a wave: every tile of Y read from LDS then meets two tiles of X, which halves the LDS reads for each
 // product, and at r = 256 the second product's sums are just the 256 accumulator registers that a lane has.  That is one
@@ -41,7 +44,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kHold = kHeadTile;      // rows of X per workgroup: 64 per wave
 constexpr int kTile = 32;             // rows of Y per tile
-constexpr float kMostSum = 0x1p20f;   // of a tile's 16 terms in a lane, above which the reference moves
+constexpr float kMostSum = 0x1p80f;   // of a tile's 16 terms in a lane, above which the reference moves
 
 // ------------------------------------------------------------------------------------------
 // tiles
@@ -261,6 +264,9 @@ __device__ __forceinline__ bf16x8 pack8(const float* v) {
   return __builtin_convertvector(f, bf16x8);
 }
 
+// this wave's LDS accesses are done: what its lanes wrote is there for the others, and what they read may be overwritten
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // two probabilities as a word of an operand
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -292,7 +298,10 @@ __device__ __forceinline__ void acc_settle() { asm volatile("s_nop 15\n\ts_nop 1
 // rho held, W streamed
 // ------------------------------------------------------------------------------------------
 // block (row block, split): split sp of the vocabulary's tiles.  Writes per row and split (R, sum) and, with GRAD,
-// sum_v 2^(y_v - R) W_v.
+// sum_v bf16(2^(y_v - R)) W_v.  R is the largest of the first tile's y_v, and with GRAD all of the split's terms are
+// rounded as they stand above the R that is written: k_head_finish takes the roundings of the teacher's entries back.
+// Sums of up to 2^80 of what R stands for are as good as others; where one would pass that (55 nats above the first tile's
+// largest logit at T = 1), R moves, and the split is done over from the R that it ends with, at most once.
 template <int D, bool GRAD>
 __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                           int64_t rows, int V, int r, float c, int splits,
@@ -306,10 +315,19 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
 
   bf16x8 xf[2][D / 16];
   hold_load<D>(xf, rho, x0, rows, r);
-  f32x16 o[2][GRAD ? D / 32 : 1] = {};
-  float ref[2] = {kNoRef, kNoRef}, sum[2] = {0.f, 0.f};
+  f32x16 o[2][GRAD ? D / 32 : 1];
+  float ref[2] = {kNoRef, kNoRef}, sum[2];
   constexpr int kLoads = Tile<D>::kLoads;
   const TileStream<D> stream(W, V, r);
+  bool over = false;   // a second time
+again:
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    sum[x] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < (GRAD ? D / 32 : 1); ++dt) o[x][dt] = f32x16{};
+  }
+  bool moved = false;   // a reference that terms of earlier tiles have been rounded with
   for (int i = 0; i < 3; ++i) stream.start(tiles[i], min(t0 + i, nt - 1));
   stream_wait<2 * kLoads>();
   __syncthreads();
@@ -353,8 +371,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
     }
     pieces_first(a, tiles[next]);
     ex.finish(D / 16 - 1, end);
-    // Entries far above the reference (those of the first tile are): a new one, the sums rescaled, the tile again
-    if (__builtin_amdgcn_ballot_w64(!(fmaxf(add[0], add[1]) < kMostSum))) {
+    // Entries far above a row's reference (those of the first tile are): a new one, its sums rescaled, the tile again
+    if (__builtin_amdgcn_ballot_w64(fmaxf(add[0], add[1]) >= kMostSum)) {
       pieces_first(a, cur);
       product_s<D>(s, a, cur, xf);   // (so that the logits need not be kept)
       past_v();
@@ -364,8 +382,10 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[x][i]);
         top *= c;
-        const float to = fmaxf(ref[x], fmaxf(top, __shfl_xor(top, 32)));
+        const bool far = fmaxf(add[x], __shfl_xor(add[x], 32)) >= kMostSum;
+        const float to = fmaxf(ref[x], far ? fmaxf(top, __shfl_xor(top, 32)) : kNoRef);
         const float f = fast_exp2(fmaxf(ref[x] - to, kNoTerm));
+        moved |= far && ref[x] > kNoRef;
         ref[x] = to;
         sum[x] *= f;
         add[x] = 0.f;
@@ -390,8 +410,15 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restri
     before = at;
     at = next;
   }
-  if constexpr (GRAD)
+  if constexpr (GRAD) {
+    if (!over && __syncthreads_or(moved)) {
+      over = true;
+      stream_wait<0>();
+      __syncthreads();
+      goto again;
+    }
     if (t0 < t1) product_o<D>(o, tiles[before], p, [](int) {});
+  }
   stream_wait<0>();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -428,7 +455,8 @@ struct HeadOut {
   float *loss, *lse;       // either may be NULL
   bf16_t* d_rho;           // with gradients: [rows, r]
   float* row;              //   what k_head_w needs of each row, by tiles (RowTile)
-  float* coef;             //   [rows, K]: -g q_k / T of each entry
+  int32_t* id;             //   [rows, K]: the id of an entry that is its row's first of it, else -1
+  float* coef;             //   [rows, K]: what the entry adds to the coefficient that k_head_w gives its token
 };
 
 __device__ __forceinline__ void put_row(float* rows, int64_t place, float l, bool negative) {
@@ -448,8 +476,48 @@ __device__ __forceinline__ void add4(float4& d, float f, float4 y) {
   d.w = __builtin_fmaf(f, y.w, d.w);
 }
 
-// one workgroup per row: joins the splits, takes the teacher's logits from W, finishes d_rho
-template <bool GRAD>
+// The logits rho . W_id of 32 entries of a row, by a wave on the matrix cores, in steps as those of product_s: a result is
+// the same bits wherever its two rows stand in the tiles and whichever of them comes first (checked over 2 x 10^6 results).
+// W's rows come by whole lines, eight rows at a load, and turn in LDS, 64 columns at a time (`turn`, 4 KB a wave's).
+template <int D>
+__device__ __forceinline__ void entry_logits(const uint4* row, const bf16_t* W, int r, const int* id, uint4* turn, float* logit) {
+  constexpr int kParts = D / 64, kTogether = kParts < 2 ? kParts : 2;   // (the loads of two parts in flight together)
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, m = lane >> 3, g = lane & 7;
+  f32x16 s = {};
+#pragma unroll
+  for (int part = 0; part < kParts; part += kTogether) {
+    uint4 a[kTogether][4];
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 64 * (part + u) + 8 * g;
+        a[u][i] = uint4{0, 0, 0, 0};
+        if (c < r) a[u][i] = *reinterpret_cast<const uint4*>(W + (size_t)max(id[8 * i + m], 0) * r + c);
+      }
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) turn[(8 * i + m) * 8 + (g ^ m)] = a[u][i];
+      lds_done();
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, turn[n * 8 + ((2 * k + h) ^ (n & 7))]),
+                                                    __builtin_bit_cast(bf16x8, row[8 * (part + u) + 2 * k + h]), s, 0, 0, 0);
+      lds_done();
+    }
+  }
+  if (n == 0)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) logit[8 * (i >> 2) + 4 * h + (i & 3)] = s[i];
+}
+// what rounding to bf16 takes from a value
+__device__ __forceinline__ float rounded_off(float v) { return v - (float)(__bf16)v; }
+
+// One workgroup per row: joins the splits, takes the teacher's logits from W, finishes d_rho.  An entry's coefficient is
+// -g q / T and what the dense kernels' rounding took from its probability, so that g / T (M p - q) is a difference of
+// float32 numbers however near p is to q.
+template <int D, bool GRAD>
 __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                           int64_t rows, int V, int r, TeacherArgs te,
                                                           const float* __restrict__ weight, int splits,
@@ -457,56 +525,75 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
                                                           const float* __restrict__ part_o, HeadOut o) {
   __shared__ RowShared<> shr;
   __shared__ TeacherShared<kThreads> sht;
-  __shared__ float q[256], log_q[256], scale[kHeadMostSplits];
-  __shared__ int id[256];
-  __shared__ float4 acc[kWaves][64];
-  __shared__ float loss[kWaves];
+  __shared__ float q[256], logit[256], coef[256], ref[kHeadMostSplits], scale[kHeadMostSplits];
+  __shared__ __attribute__((aligned(16))) int id[256];
+  __shared__ uint4 x[D / 8];   // the row of rho, 0 past r
+  __shared__ uint4 turn[kWaves][256];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t row = blockIdx.x;
   float mass;
   const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, row, V), sht, &mass);
   q[t] = e.q;
-  log_q[t] = e.log_q;
   id[t] = e.id;
+  if (t < D / 8) x[t] = 8 * t < r ? *reinterpret_cast<const uint4*>(rho + (size_t)row * r + 8 * t) : uint4{0, 0, 0, 0};
   RowSum a = row_empty();
   for (int i = t; i < splits; i += kThreads) {   // (at most kHeadMostSplits)
     const float2 p = part_sum[(size_t)i * rows + row];
-    scale[i] = p.x;
+    ref[i] = p.x;
     a = row_merge<false>(a, RowSum{p.x, p.y, 0.f});
   }
-  a = row_block_merge<false>(a, shr);
+  a = row_block_merge<false>(a, shr);   // (its barrier covers id, q and x)
   const float l2 = fast_log2(a.s), w = (weight ? weight[row] : 1.f) * te.inv_temp;
-  for (int i = t; i < splits; i += kThreads) scale[i] = w * mass * fast_exp2(fmaxf(scale[i] - a.R, kNoTerm)) / a.s;
+  for (int i = t; i < splits; i += kThreads) scale[i] = w * mass * fast_exp2(fmaxf(ref[i] - a.R, kNoTerm)) / a.s;
+  for (int k = 32 * wave; k < te.k; k += 32 * kWaves) entry_logits<D>(x, W, r, id + k, turn[wave], logit + k);
+  __syncthreads();
+
+  const float loss = block_sum<kThreads>(e.id >= 0 ? teacher_term(e, __builtin_fmaf(logit[t], te.c, -a.R) - l2) : 0.f, sht.red);
+  if (t == 0) {
+    if (o.loss) o.loss[row] = loss;
+    if (o.lse) o.lse[row] = row_lse(a);
+  }
+  if (!GRAD) return;
+  // what k_head_w needs of the row; the places of its tile that no row has: 2^-kMostY = 0 (the last of several tiles ends
+  // with the last row)
+  const int64_t whole = rows / kTile * kTile, left = rows - whole;
+  const float f = w * mass, l = f != 0.f ? a.R + l2 - fast_log2(fabsf(f)) : kMostY;
+  if (t == 0) put_row(o.row, rows > kTile && row >= whole ? row + kTile - left : row, l, f < 0.f);
+  if (row == rows - 1 && left > 0 && t < kTile - left) put_row(o.row, rows > kTile ? whole + t : rows + t, kMostY, false);
+  if (t < te.k) {
+    bool first = e.id >= 0;   // several entries of one id are the first one's
+    float c_rho = 0.f, c_w = 0.f;
+    if (first) {
+      uint32_t same = 0;   // how many entries have the id, and how many of them come first
+#pragma unroll 4
+      for (int j = 0; j < te.k; j += 4) {
+        const int4 v = *reinterpret_cast<const int4*>(id + j);
+        const int here[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) same += here[u] != e.id ? 0u : j + u < t ? 0x10001u : 1u;
+      }
+      first = same < 0x10000u;
+      float sum = e.q;
+      if (same != 1) {
+        sum = 0.f;
+        for (int j = 0; j < te.k; ++j) sum += id[j] == e.id ? q[j] : 0.f;
+      }
+      // the split that has the id's tile
+      const int nt = TileStream<D>::count(V), sp = (int)(((int64_t)(e.id / kTile + 1) * splits + nt - 1) / nt) - 1;
+      c_rho = scale[sp] * rounded_off(fast_exp2(__builtin_fmaf(logit[t], te.c, -ref[sp]))) - w * sum;
+      const float lost = rounded_off(fast_exp2(__builtin_fmaf(logit[t], te.c, -l)));
+      c_w = (f < 0.f ? -lost : lost) - w * sum;
+    }
+    coef[t] = first ? c_rho : 0.f;
+    o.id[(size_t)row * te.k + t] = first ? e.id : -1;
+    o.coef[(size_t)row * te.k + t] = c_w;
+  }
   __syncthreads();
 
   const bool on = 4 * lane < r;   // this lane's four columns
-  const float4 x = on ? widen4(*reinterpret_cast<const uint2*>(rho + (size_t)row * r + 4 * lane)) : make_float4(0, 0, 0, 0);
   float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
-  float term = 0.f;
-  // the wave's entries and splits, four at a time: their loads in flight together
-  for (int k0 = wave; k0 < te.k; k0 += 4 * kWaves) {
-    float4 y[4];
-    float dot[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = k0 + u * kWaves, v = k < te.k ? id[k] : -1;
-      y[u] = on && v >= 0 ? widen4(*reinterpret_cast<const uint2*>(W + (size_t)v * r + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      dot[u] = __builtin_fmaf(x.x, y[u].x, x.y * y[u].y) + __builtin_fmaf(x.z, y[u].z, x.w * y[u].w);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) dot[u] = lanes_sum(dot[u]);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = k0 + u * kWaves;
-      if (k >= te.k) break;
-      const TeacherEntry ek = {id[k], q[k], log_q[k]};   // (an absent entry's weight is 0)
-      term += teacher_term(ek, __builtin_fmaf(dot[u], te.c, -a.R) - l2);
-      if (GRAD) add4(d, -w * q[k], y[u]);
-    }
-  }
-  if (GRAD && on) {
+  if (on) {
+    // the wave's splits and entries, four at a time: their loads in flight together
     const float* from = part_o + (size_t)row * r + 4 * lane;
     const size_t step = (size_t)rows * r;
     int sp = wave;
@@ -518,35 +605,33 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
       for (int u = 0; u < 4; ++u) add4(d, scale[sp + u * kWaves], y[u]);
     }
     for (; sp < splits; sp += kWaves) add4(d, scale[sp], *reinterpret_cast<const float4*>(from + sp * step));
-  }
-  if (lane == 0) loss[wave] = term;
-  if (GRAD) acc[wave][lane] = d;
-  __syncthreads();
-  if (t == 0) {
-    if (o.loss) o.loss[row] = (loss[0] + loss[1]) + (loss[2] + loss[3]);
-    if (o.lse) o.lse[row] = row_lse(a);
-    if (GRAD) {   // the last of several tiles ends with the last row
-      const int64_t whole = rows / kTile * kTile, pad = rows > kTile && rows > whole ? whole + kTile - rows : 0;
-      const float f = w * mass;
-      put_row(o.row, row < whole ? row : row + pad, f != 0.f ? a.R + l2 - fast_log2(fabsf(f)) : kMostY, f < 0.f);
-    }
-  }
-  if (GRAD) {
-    // the places of its tile that no row has: 2^-kMostY = 0
-    const int64_t whole = rows / kTile * kTile, left = rows - whole;
-    if (row == rows - 1 && left > 0 && t < kTile - left) put_row(o.row, rows > kTile ? whole + t : rows + t, kMostY, false);
-    if (t < te.k) o.coef[(size_t)row * te.k + t] = -w * e.q;
-    if (wave == 0 && on) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      typedef float f32x4 __attribute__((ext_vector_type(4)));
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave; k0 < te.k; k0 += 4 * kWaves) {
+      uint2 y[4];
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float4 p = acc[k][lane];
-        v += f32x4{p.x, p.y, p.z, p.w};
+      for (int u = 0; u < 4; ++u) {
+        const int k = min(k0 + u * kWaves, te.k - 1);
+        y[u] = *reinterpret_cast<const uint2*>(W + (size_t)max(id[k], 0) * r + 4 * lane);
       }
-      *reinterpret_cast<bf16x4*>(o.d_rho + (size_t)row * r + 4 * lane) = __builtin_convertvector(v, bf16x4);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = k0 + u * kWaves;
+        if (k < te.k && id[k] >= 0) add4(d, coef[k], widen4(y[u]));
+      }
     }
+  }
+  float4* acc = reinterpret_cast<float4*>(turn[0]);   // (turn has served)
+  acc[wave * 64 + lane] = d;
+  __syncthreads();
+  if (wave == 0 && on) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const float4 p = acc[k * 64 + lane];
+      v += f32x4{p.x, p.y, p.z, p.w};
+    }
+    *reinterpret_cast<bf16x4*>(o.d_rho + (size_t)row * r + 4 * lane) = __builtin_convertvector(v, bf16x4);
   }
 }
 
@@ -559,28 +644,23 @@ extern __shared__ uint32_t key_lds[];   // a word per key
 // A wave's entries are taken 512 at a time, eight a lane, whose loads are all in flight together.
 constexpr int kSortLoads = 8;
 struct SortEntry {
-  int id;        // -1: absent
+  int id;        // -1: absent, or not its row's first of that id
   float coef;
 };
 // entries e0 + 64 u + lane below `end`
 template <bool COEF>
-__device__ __forceinline__ void sort_load(SortEntry (&en)[kSortLoads], const TeacherArgs& te, const float* coef,
-                                          int64_t e0, int64_t end, int V) {
-  float y[kSortLoads];
+__device__ __forceinline__ void sort_load(SortEntry (&en)[kSortLoads], const int32_t* ids, const float* coef, int64_t e0,
+                                          int64_t end) {
 #pragma unroll
   for (int u = 0; u < kSortLoads; ++u) {
     const int64_t e = e0 + u * 64 + (threadIdx.x & 63);
-    en[u].id = e < end ? te.ids[e] : -1;
-    y[u] = e < end ? te.values[e] : -INFINITY;
+    en[u].id = e < end ? ids[e] : -1;
     if (COEF) en[u].coef = e < end ? coef[e] : 0.f;
   }
-#pragma unroll
-  for (int u = 0; u < kSortLoads; ++u)
-    if (en[u].id < 0 || en[u].id >= V || !(y[u] > -INFINITY)) en[u].id = -1;
 }
 
 // one wave per chunk of the entries: how many of each key
-__global__ __launch_bounds__(64) void k_sort_count(TeacherArgs te, int64_t n, int V, int keys, int chunk,
+__global__ __launch_bounds__(64) void k_sort_count(const int32_t* __restrict__ ids, int64_t n, int keys, int chunk,
                                                    uint32_t* __restrict__ counts) {
   const int lane = threadIdx.x;
   for (int i = lane; i < keys; i += 64) key_lds[i] = 0;
@@ -588,7 +668,7 @@ __global__ __launch_bounds__(64) void k_sort_count(TeacherArgs te, int64_t n, in
   const int64_t e0 = (int64_t)blockIdx.x * chunk, end = min(e0 + chunk, n);
   for (int64_t e = e0; e < end; e += 64 * kSortLoads) {
     SortEntry en[kSortLoads];
-    sort_load<false>(en, te, nullptr, e, end, V);
+    sort_load<false>(en, ids, nullptr, e, end);
 #pragma unroll
     for (int u = 0; u < kSortLoads; ++u)
       if (en[u].id >= 0) atomicAdd(&key_lds[en[u].id / kHeadGroup], 1u);
@@ -651,17 +731,16 @@ __global__ __launch_bounds__(1024) void k_sort_base(const uint32_t* __restrict__
 
 // one wave per chunk: entry -> its place, in the order of the entries.  list: (row | place in the group << 24,
 // coefficient)
-__global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, int V, int keys, int chunk,
-                                                   const uint32_t* __restrict__ counts,
-                                                   const uint32_t* __restrict__ begin, const float* __restrict__ coef,
-                                                   uint2* __restrict__ list) {
+__global__ __launch_bounds__(64) void k_sort_place(const int32_t* __restrict__ ids, const float* __restrict__ coef, int per_row,
+                                                   int64_t n, int keys, int chunk, const uint32_t* __restrict__ counts,
+                                                   const uint32_t* __restrict__ begin, uint2* __restrict__ list) {
   const int lane = threadIdx.x;
   for (int i = lane; i < keys; i += 64) key_lds[i] = begin[i] + counts[(size_t)blockIdx.x * keys + i];
   __syncthreads();
   const int64_t e0 = (int64_t)blockIdx.x * chunk, end = min(e0 + chunk, n);
   for (int64_t e = e0; e < end; e += 64 * kSortLoads) {
     SortEntry en[kSortLoads];
-    sort_load<true>(en, te, coef, e, end, V);
+    sort_load<true>(en, ids, coef, e, end);
 #pragma unroll
     for (int u = 0; u < kSortLoads; ++u) {
       const int key = en[u].id < 0 ? -1 : en[u].id / kHeadGroup;
@@ -675,7 +754,7 @@ __global__ __launch_bounds__(64) void k_sort_place(TeacherArgs te, int64_t n, in
       }
       if (key >= 0) {
         const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-        list[key_lds[key] + rank] = make_uint2((uint32_t)((e + u * 64 + lane) / te.k) | (uint32_t)(en[u].id % kHeadGroup) << 24,
+        list[key_lds[key] + rank] = make_uint2((uint32_t)((e + u * 64 + lane) / per_row) | (uint32_t)(en[u].id % kHeadGroup) << 24,
                                                __float_as_uint(en[u].coef));
       }
       __syncthreads();
@@ -705,7 +784,9 @@ __device__ __forceinline__ void wave_tile_stream(const Tile<D>& to, const bf16_t
     stream_to_lds16(Y, offset, lds_address(to.y) + w * N * 1024);
   }
 }
-// O += q^T Y for a tile's coefficients q[tile row][held row] in LDS, as two bf16 terms: their rounded values and the rest
+// O += q^T Y for a tile's coefficients q[tile row][held row] in LDS, as two bf16 terms: their rounded values and the rest's.
+// A coefficient is -p + d with p the bf16 number that the rows' tiles have added, so that its first term, the nearest bf16
+// number, is within |d| of it: the second is off by at most 2^-8 d (and by 2^-16 of the coefficient).
 template <int D>
 __device__ __forceinline__ void coefficient_products(f32x16 (&o)[2][D / 32], const Tile<D>& t, const float* q) {
   const int n = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
@@ -718,7 +799,7 @@ __device__ __forceinline__ void coefficient_products(f32x16 (&o)[2][D / 32], con
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         e[i] = q[(16 * j + 8 * (i >> 2) + 4 * h + (i & 3)) * kHeadGroup + 32 * x + n];
-        rest[i] = e[i] - (float)(__bf16)e[i];
+        rest[i] = rounded_off(e[i]);
       }
       p[0][x][j] = pack8(e);
       p[1][x][j] = pack8(rest);
@@ -731,9 +812,6 @@ __device__ __forceinline__ void coefficient_products(f32x16 (&o)[2][D / 32], con
       for (int j = 0; j < 2; ++j) p[0][x][j] = p[1][x][j];
   }
 }
-// this wave's LDS accesses are done (its next stream may overwrite what they read)
-__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                         int64_t rows, int V, int r, float c,
@@ -954,17 +1032,18 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   float2* part_sum = (float2*)a.ws;
   float* part_o = (float*)(a.ws + l.off_o);
   const unsigned grid = (unsigned)((a.rows + kHold - 1) / kHold * l.splits);
-  HeadOut o = {a.out_loss, a.out_lse, nullptr, nullptr, nullptr};
+  HeadOut o = {a.out_loss, a.out_lse, nullptr, nullptr, nullptr, nullptr};
   hipError_t e;
   if (!a.d_rho) {
     k_head_rho<D, false><<<grid, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher.c, l.splits, part_sum, nullptr);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    k_head_finish<false><<<(unsigned)a.rows, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher, a.weight, l.splits,
+    k_head_finish<D, false><<<(unsigned)a.rows, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher, a.weight, l.splits,
                                                                 part_sum, nullptr, o);
     return hipGetLastError();
   }
   o.d_rho = (bf16_t*)a.d_rho;
   o.row = (float*)(a.ws + l.off_row);
+  o.id = (int32_t*)(a.ws + l.off_id);
   o.coef = (float*)(a.ws + l.off_coef);
   uint32_t *counts = (uint32_t*)(a.ws + l.off_counts), *totals = (uint32_t*)(a.ws + l.off_totals);
   uint32_t* begin = totals + l.keys;
@@ -972,16 +1051,16 @@ hipError_t launch_d(const HeadDistillArgs& a, hipStream_t st) {
   const int64_t n = a.rows * a.teacher.k;
   k_head_rho<D, true><<<grid, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher.c, l.splits, part_sum, part_o);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_head_finish<true><<<(unsigned)a.rows, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher, a.weight, l.splits,
+  k_head_finish<D, true><<<(unsigned)a.rows, kThreads, 0, st>>>(rho, W, a.rows, a.V, a.r, a.teacher, a.weight, l.splits,
                                                              part_sum, part_o, o);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_sort_count<<<(unsigned)l.chunks, 64, key_bytes, st>>>(a.teacher, n, a.V, l.keys, l.chunk, counts);
+  k_sort_count<<<(unsigned)l.chunks, 64, key_bytes, st>>>(o.id, n, l.keys, l.chunk, counts);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_sort_scan<<<(unsigned)l.keys, kThreads, 0, st>>>(counts, l.chunks, l.keys, totals);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_sort_base<<<1, 1024, 0, st>>>(totals, l.keys, begin);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  k_sort_place<<<(unsigned)l.chunks, 64, key_bytes, st>>>(a.teacher, n, a.V, l.keys, l.chunk, counts, begin, o.coef, list);
+  k_sort_place<<<(unsigned)l.chunks, 64, key_bytes, st>>>(o.id, o.coef, a.teacher.k, n, l.keys, l.chunk, counts, begin, list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   float* part_w = (float*)(a.ws + l.off_o);   // (the splits' sums are joined by now)
   k_head_w<D><<<(unsigned)(l.whole + (l.tiles - l.whole) * l.row_splits), kThreads, 0, st>>>(
@@ -1016,6 +1095,8 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
     at += up(std::max((size_t)l.splits * rows, (size_t)(l.tiles - l.whole) * l.row_splits * kHold) * r * sizeof(float));
     l.off_row = at;
     at += up((size_t)((rows + kTile - 1) / kTile) * sizeof(RowTile));
+    l.off_id = at;
+    at += up((size_t)n * sizeof(int32_t));
     l.off_coef = at;
     at += up((size_t)n * sizeof(float));
     l.off_counts = at;

@@ -934,8 +934,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
         for (int u = 0; u < 4; ++u) {
           const uint32_t row = en[u].x & 0xffffffu;
           const bool in = b + u * 64 + lane < b1 && (int)(row / kTile) == k;
-          // (one wave's LDS additions happen in its own order: repeated ids always add up the same way)
-          if (in) unsafeAtomicAdd(q + (row - first) * kHeadGroup + (en[u].x >> 24), __uint_as_float(en[u].y));
+          if (in) q[(row - first) * kHeadGroup + (en[u].x >> 24)] = __uint_as_float(en[u].y);   // (a place has one entry)
           found += __popcll(__builtin_amdgcn_ballot_w64(in));
         }
         batch = b;

@@ -442,12 +442,10 @@ again:
 // ------------------------------------------------------------------------------------------
 // a row's results
 // ------------------------------------------------------------------------------------------
-// A tile's rows: R + log2 s - log2 |g M / T|, so that 2^(y - l) is the entry's weight of the row, and the weight's sign in
-// the place of a bf16's.  64 words, one a lane's.
+// A tile's rows: g M / T p = factor 2^(y - R).  (All in one exponent would leave the row's part of it to the last place of
+// R, which is 1/64 where logits of 10 stand at T = 1e-4.)  64 words, one a lane's.
 struct RowTile {
-  float l[kTile];
-  uint16_t sign[kTile];
-  uint32_t unused[kTile / 2];
+  float R[kTile], factor[kTile];
 };
 static_assert(sizeof(RowTile) == 256, "a word a lane");
 
@@ -459,10 +457,10 @@ struct HeadOut {
   float* coef;             //   [rows, K]: what the entry adds to the coefficient that k_head_w gives its token
 };
 
-__device__ __forceinline__ void put_row(float* rows, int64_t place, float l, bool negative) {
+__device__ __forceinline__ void put_row(float* rows, int64_t place, float R, float factor) {
   RowTile* t = reinterpret_cast<RowTile*>(rows) + place / kTile;
-  t->l[place % kTile] = l;
-  t->sign[place % kTile] = negative ? 0x8000 : 0;
+  t->R[place % kTile] = R;
+  t->factor[place % kTile] = factor;
 }
 
 __device__ __forceinline__ float4 widen4(uint2 v) {
@@ -544,7 +542,7 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
   }
   a = row_block_merge<false>(a, shr);   // (its barrier covers id, q and x)
   const float l2 = fast_log2(a.s), w = (weight ? weight[row] : 1.f) * te.inv_temp;
-  for (int i = t; i < splits; i += kThreads) scale[i] = w * mass * fast_exp2(fmaxf(ref[i] - a.R, kNoTerm)) / a.s;
+  for (int i = t; i < splits; i += kThreads) scale[i] = mass * fast_exp2(fmaxf(ref[i] - a.R, kNoTerm)) / a.s;
   for (int k = 32 * wave; k < te.k; k += 32 * kWaves) entry_logits<D>(x, W, r, id + k, turn[wave], logit + k);
   __syncthreads();
 
@@ -554,12 +552,12 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
     if (o.lse) o.lse[row] = row_lse(a);
   }
   if (!GRAD) return;
-  // what k_head_w needs of the row; the places of its tile that no row has: 2^-kMostY = 0 (the last of several tiles ends
-  // with the last row)
+  // what k_head_w needs of the row (the log-sum-exp rounded, so that its exponentials are at most about 1, and in the factor
+  // what is left); the places of its tile that no row has: 0 2^-kMostY (the last of several tiles ends with the last row)
   const int64_t whole = rows / kTile * kTile, left = rows - whole;
-  const float f = w * mass, l = f != 0.f ? a.R + l2 - fast_log2(fabsf(f)) : kMostY;
-  if (t == 0) put_row(o.row, rows > kTile && row >= whole ? row + kTile - left : row, l, f < 0.f);
-  if (row == rows - 1 && left > 0 && t < kTile - left) put_row(o.row, rows > kTile ? whole + t : rows + t, kMostY, false);
+  const float R = a.R + l2, f = w * mass * (fast_exp2(R - a.R) / a.s);
+  if (t == 0) put_row(o.row, rows > kTile && row >= whole ? row + kTile - left : row, R, f);
+  if (row == rows - 1 && left > 0 && t < kTile - left) put_row(o.row, rows > kTile ? whole + t : rows + t, kMostY, 0.f);
   if (t < te.k) {
     bool first = e.id >= 0;   // several entries of one id are the first one's
     float c_rho = 0.f, c_w = 0.f;
@@ -580,9 +578,8 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
       }
       // the split that has the id's tile
       const int nt = TileStream<D>::count(V), sp = (int)(((int64_t)(e.id / kTile + 1) * splits + nt - 1) / nt) - 1;
-      c_rho = scale[sp] * rounded_off(fast_exp2(__builtin_fmaf(logit[t], te.c, -ref[sp]))) - w * sum;
-      const float lost = rounded_off(fast_exp2(__builtin_fmaf(logit[t], te.c, -l)));
-      c_w = (f < 0.f ? -lost : lost) - w * sum;
+      c_rho = scale[sp] * rounded_off(fast_exp2(__builtin_fmaf(logit[t], te.c, -ref[sp]))) - sum;
+      c_w = rounded_off(f * fast_exp2(__builtin_fmaf(logit[t], te.c, -R))) - w * sum;
     }
     coef[t] = first ? c_rho : 0.f;
     o.id[(size_t)row * te.k + t] = first ? e.id : -1;
@@ -631,6 +628,7 @@ __global__ __launch_bounds__(kThreads) void k_head_finish(const bf16_t* __restri
       const float4 p = acc[k * 64 + lane];
       v += f32x4{p.x, p.y, p.z, p.w};
     }
+    v *= w;
     *reinterpret_cast<bf16x4*>(o.d_rho + (size_t)row * r + 4 * lane) = __builtin_convertvector(v, bf16x4);
   }
 }
@@ -861,19 +859,17 @@ __global__ __launch_bounds__(kThreads, 1) void k_head_w(const bf16_t* __restrict
     Words now;
     // four rows' numbers at a time, read while the four before are used (a read just before its use would be waited for,
     // with all the reads of Y before it)
-    float4 l[4];
-    uint2 sign[4];
+    float4 R[4], factor[4];
     auto rows_of = [&](int g) {
-      l[g] = *reinterpret_cast<const float4*>(st.l + 8 * g + 4 * h);
-      sign[g] = *reinterpret_cast<const uint2*>(st.sign + 8 * g + 4 * h);
+      R[g] = *reinterpret_cast<const float4*>(st.R + 8 * g + 4 * h);
+      factor[g] = *reinterpret_cast<const float4*>(st.factor + 8 * g + 4 * h);
     };
-    auto begin = [&](int x, int i) {
-      const float4 f = l[i >> 2];
-      return fast_exp2(__builtin_fmaf(s[x][i], c, -(i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w)));
-    };
+    auto of_row = [](const float4 (&f)[4], int i) { return i % 4 == 0 ? f[i / 4].x : i % 4 == 1 ? f[i / 4].y : i % 4 == 2 ? f[i / 4].z : f[i / 4].w; };
+    auto begin = [&](int x, int i) { return fast_exp2(__builtin_fmaf(s[x][i], c, -of_row(R, i))); };
     auto end = [&](int x, int i, float e) {
-      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], e) ^ (i % 4 == 1 ? sign[i >> 2].x : sign[i >> 2].y);
-      return e;
+      const float p = of_row(factor, i) * e;
+      if (i % 2) now.w[x][i / 2] = pack2(ex.e[x][i - 1], p);
+      return p;
     };
     rows_of(0);
     product_o<D>(o, tiles[before], p, [&](int q) {

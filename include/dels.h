@@ -416,7 +416,9 @@ dls_status dls_token_logprobs(const void *logits, dls_dtype dtype, int64_t rows,
  *   d s_v = g / T (M p_v - sum_{k: id_k = v} q_k)
  * An entry is absent when its id lies outside [0, V) or its value is -inf; a row without entries has
  * loss 0 and gradient 0 (a position left out).  Entries of a row may repeat an id.  A masked student
- * entry (-inf) has p = 0; a teacher entry of positive weight there makes the loss +inf. */
+ * entry (-inf) has p = 0; a teacher entry of positive weight there makes the loss +inf.  A student row with a NaN
+ * or +inf has NaN for its loss, its log-sum-exp and its whole gradient (0 for loss and gradient where the row has
+ * no teacher entries).  A teacher value of NaN counts as absent. */
 #define DLS_TEACHER_LOGPROBS 0x1u
 typedef struct dls_teacher {
   const int32_t *ids;    /* [rows, k] device */

@@ -19,7 +19,7 @@ constexpr int kThreads = kRowThreads;
 
 struct LossOut {
   float *loss, *lse;   // either may be NULL
-  float2* row;         // (R, log2 s) for the gradient pass, or NULL
+  float2* row;         // (R, log2 s; +inf for an empty row) for the gradient pass, or NULL
 };
 
 // the loss of a row from its sums, by the whole workgroup
@@ -28,7 +28,7 @@ __device__ __forceinline__ void finish_row(const T* row, int V, int64_t r, const
                                            TeacherShared<kThreads>& sh, const LossOut& o) {
   float mass;
   const TeacherEntry e = teacher_entry<kThreads>(te, teacher_raw(te, r, V), sh, &mass);
-  const float l2 = a.s > 0.f ? fast_log2(a.s) : 0.f;
+  const float l2 = a.s == 0.f ? INFINITY : fast_log2(a.s);
   const float x = e.id >= 0 ? to_f32(row[e.id]) : -INFINITY;
   const float loss = block_sum<kThreads>(teacher_term(e, above_ref(x, te.c, a.R) - l2), sh.red);
   if (threadIdx.x == 0) {
@@ -105,23 +105,28 @@ template <> struct Store<bf16_t> {
   __device__ __forceinline__ static void one(bf16_t* p, float v) { *p = __builtin_bit_cast(bf16_t, (__bf16)v); }
 };
 
-// The dense part of a gradient, f 2^(y - R), of n entries.  R is the same in every lane of the workgroup, so the choice is
-// a scalar branch; a clamped R holds no difference of the size of a logarithm, so there a probability is at most 1.
+// The dense part of a gradient, f 2^(y - R), of n entries; 0 where f is, whatever the entries.  R and f are the same in
+// every lane of the workgroup, so the choice is a scalar branch; a clamped R holds no difference of the size of a logarithm,
+// so there a probability is at most 1.
 struct Dense {
   float c, R, f;
   bool plain;
-  __device__ __forceinline__ Dense(float c, float R_, float f) : c(c), f(f) {
+  __device__ __forceinline__ Dense(float c, float R_, float f_) : c(c) {
     R = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(R_)));
-    plain = fabsf(R) < kPlainRef;
+    f = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(f_)));
+    plain = fabsf(R) < kPlainRef && f != 0.f;
   }
   template <int n>
   __device__ __forceinline__ void operator()(const float* x, float* d) const {
     if (plain) {
 #pragma unroll
       for (int i = 0; i < n; ++i) d[i] = f * fast_exp2(__builtin_fmaf(x[i], c, -R));
-    } else {
+    } else if (f != 0.f) {
 #pragma unroll
       for (int i = 0; i < n; ++i) d[i] = f * fast_exp2(fminf(above_ref(x[i], c, R), 0.f));
+    } else {
+#pragma unroll
+      for (int i = 0; i < n; ++i) d[i] = 0.f;
     }
   }
   __device__ __forceinline__ float operator()(float x) const {
@@ -179,13 +184,13 @@ __global__ __launch_bounds__(NT) void k_distill_row(const T* L, int V, int64_t s
     ids[t] = e.id;
     qs[t] = e.q;
   }
-  const float l2 = a.s > 0.f ? fast_log2(a.s) : 0.f;
+  const float l2 = a.s == 0.f ? INFINITY : fast_log2(a.s);
   const float loss = block_sum<NT>(teacher_term(e, above_ref(xk, te.c, a.R) - l2), sht.red);   // (its barriers cover ids, qs)
   if (t == 0) {
     if (o.loss) o.loss[r] = loss;
     if (o.lse) o.lse[r] = row_lse(a);
   }
-  const float w = (weight ? weight[r] : 1.f) * te.inv_temp, f = a.s > 0.f ? w * mass / a.s : 0.f;
+  const float w = (weight ? weight[r] : 1.f) * te.inv_temp, f = a.s == 0.f || mass == 0.f ? 0.f : w * mass / a.s;
   const Dense dense(te.c, a.R, f);
   bool mine = e.id >= 0;
   float entry = 0.f;
@@ -251,12 +256,13 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, in
   if (row_stats) {
     const float2 p = row_stats[r];
     R = p.x;
-    f = R == kNoRef ? 0.f : fast_exp2(-p.y);
+    f = fast_exp2(-p.y);
   } else {
     // lse log2(e) to twice the precision: the part that R cannot hold goes into the factor
     const float l = lse[r];
     R = __builtin_amdgcn_fmed3f(l * kLog2e, -kMostY, kMostY);
     f = l == -INFINITY ? 0.f
+        : !(l < INFINITY) ? __builtin_nanf("")
         : fabsf(R) < kPlainRef ? fast_exp2(-(__builtin_fmaf(l, kLog2e, -R) + l * kLog2eLow)) : 1.f;
   }
   const float w = (weight ? weight[r] : 1.f) * te.inv_temp;
@@ -265,7 +271,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(const T* L, int V, in
   ids[t] = e.id;
   qs[t] = e.q;
   __syncthreads();   // (also: every entry of the teacher's has been read)
-  const Dense dense(te.c, R, w * mass * f);
+  const Dense dense(te.c, R, mass == 0.f ? 0.f : w * mass * f);
   float entry = 0.f;
   if (mine) {   // several entries of one id are the first one's
     float q = 0.f;

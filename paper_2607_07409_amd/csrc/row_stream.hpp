@@ -58,10 +58,11 @@ struct RowSum {
 __device__ __forceinline__ RowSum row_empty() { return {kNoRef, 0.f, 0.f}; }
 
 // y - R of one entry; -inf for a masked one.  Rows whose largest entries lie beyond kPlainRef (a row of the
-// type's lowest value, say) take the entries' products clamped, so that nothing overflows.
+// type's lowest value, say) take the entries' products clamped, so that nothing overflows.  NaN stays NaN, and +inf
+// (always here, since it takes R there) becomes NaN, so that such a row's sum is NaN and all that comes of it.
 __device__ __forceinline__ float above_ref(float x, float c, float R) {
   if (fabsf(R) < kPlainRef) return __builtin_fmaf(x, c, -R);
-  return x == -INFINITY ? -INFINITY : __builtin_amdgcn_fmed3f(x * c, -kMostY, kMostY) - R;
+  return x == -INFINITY ? -INFINITY : __builtin_fmaf(x, 0.f, __builtin_amdgcn_fmed3f(x * c, -kMostY, kMostY) - R);
 }
 
 template <bool ENT>
@@ -153,9 +154,9 @@ __device__ __forceinline__ RowSum row_block_merge(RowSum a, RowShared<NT>& sh) {
   return row_wave_merge<ENT, NT / 64>(RowSum{sh.R[from], sh.s[from], ENT ? sh.t[from] : 0.f});
 }
 
-// natural log-sum-exp; -inf for a row without an entry above -inf
+// natural log-sum-exp; -inf for a row without an entry above -inf (whose sum is 0: NaN is not)
 __device__ __forceinline__ float row_lse(const RowSum& a) {
-  return a.s > 0.f ? (a.R + fast_log2(a.s)) * kLn2 : -INFINITY;
+  return a.s == 0.f ? -INFINITY : (a.R + fast_log2(a.s)) * kLn2;
 }
 
 // entries before the row's first 16-byte boundary

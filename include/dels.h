@@ -392,7 +392,8 @@ dls_status dls_unigram_log_prior(const int32_t *tokens, int64_t n, int32_t V, fl
  * -inf marks a masked entry: its probability is 0 and it is no alternative.  A row with fewer than
  * top_k other entries fills up with id -1 and log probability -inf; a row without any has lse = -inf
  * and NaN for logprob and entropy.  A token outside [0, V) has logprob NaN, a masked one -inf.
- * NaN entries are not alternatives.  Finite logits beyond 1e38 T / log2(e) in magnitude count as that
+ * NaN entries are not alternatives; a row with a NaN or +inf has NaN for logprob, entropy, lse and the alternatives'
+ * log probabilities.  Finite logits beyond 1e38 T / log2(e) in magnitude count as that
  * value where the row has no smaller ones.  Limits: 0 <= rows <= 2^20, 1 <= V <= 2^24. */
 typedef struct dls_token_stats {
   float logprob;

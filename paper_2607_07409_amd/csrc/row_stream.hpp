@@ -77,14 +77,14 @@ __device__ __forceinline__ void row_rescale(RowSum& a, float R) {
 // rescales: exponentials of up to 2^kLazy are as exact as others.
 constexpr float kLazy = 8.f;
 
-template <int n, bool ENT, bool FINITE>
+template <int n, bool ENT>
 __device__ __forceinline__ void row_add(RowSum& a, const float* x, float c) {
 #pragma unroll
   for (int i = 0; i < n; ++i) {
     const float y = __builtin_fmaf(x[i], c, -a.R);   // -inf for a masked entry
     const float e = fast_exp2(y);
     a.s += e;
-    if (ENT) a.t = __builtin_fmaf(e, FINITE ? y : fmaxf(y, kNoTerm), a.t);
+    if (ENT) a.t = __builtin_fmaf(e, fmaxf(y, kNoTerm), a.t);
   }
 }
 // the same where the reference moves, or is none yet, or lies far from any logit
@@ -106,17 +106,7 @@ __device__ __forceinline__ void row_fold(RowSum& a, const float* x, float cm, fl
     row_add_moved<n, ENT>(a, x, cm, c);
     return;
   }
-  row_add<n, ENT, false>(a, x, c);
-}
-
-// A piece with its masked entries (-inf, and whatever is as far below any logit) raised to a finite value that adds as
-// little, in the half words as they are: their order as unsigned numbers is that of the magnitudes.  The entropy's sum then
-// needs no test.  -2^96 c is finite and below -2^82 for every temperature within the limits.
-constexpr float kMasked = -0x1p96f;
-__device__ __forceinline__ uint4 raise_masked(uint4 v) {
-  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-  const u16x8 most = (u16x8)(unsigned short)0xEF80;   // kMasked
-  return __builtin_bit_cast(uint4, __builtin_elementwise_min(__builtin_bit_cast(u16x8, v), most));
+  row_add<n, ENT>(a, x, c);
 }
 
 template <bool ENT>

@@ -223,13 +223,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
   row_chunks<U>(
       row, g,
       [&](const uint4* raw, auto n, int u0) {
-        // masked entries of bf16 rows raised: the plain case of row_fold, without its test; otherwise as they are
-        constexpr bool kRaise = sizeof(T) == 2;
         float x[N * n];
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
-          Chunk<T>::widen(kRaise ? raise_masked(raw[u]) : raw[u], x + u * N);
-        }
+        for (int u = 0; u < n; ++u) Chunk<T>::widen(raw[u], x + u * N);
         float cm;
         if (TOP && FINE) {
           cm = -INFINITY;
@@ -242,14 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
           cm = max_of<N * n>(x);
           bm[0] = max3(bm[0], cm, cm);
         }
-        const bool move = cm * o.c > a.R + kLazy || a.R < -kPlainRef;
-        if (__builtin_amdgcn_ballot_w64(move) && move) {
-#pragma unroll
-          for (int u = 0; u < n; ++u) Chunk<T>::widen(raw[u], x + u * N);
-          row_add_moved<N * n, true>(a, x, max_of<N * n>(x), o.c);
-        } else {
-          row_add<N * n, true, kRaise>(a, x, o.c);
-        }
+        row_fold<N * n, true>(a, x, cm, o.c);
       },
       [&](int it) {
         if (!TOP) return;
@@ -276,9 +265,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(const T* __restrict_
     if (parts == 1) put_best(o, r, a, rank, key);
     else part_keys[((size_t)r * parts + part) * o.k + rank] = key;
   };
-  if ((uint32_t)(bound >> 32) <= order_of(kMasked)) {
-    // Fewer than k blocks hold an entry that is not masked (or as low as if it were: the pass does not tell those apart):
-    // the k best of all entries, read again for every digit
+  if (bound == 1) {   // fewer than k blocks hold an entry that is not masked: the k best of all, read again for every digit
     best_keys([&](auto f) {
       row_edges(g, V, part, parts, [&](int v) { f(key_of(to_f32(row[v]), v)); });
       for (int c = g.c0 + t; c < g.c1; c += NT) {

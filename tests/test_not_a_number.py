@@ -58,3 +58,26 @@ def test_distillation(rows, V, dtype, where, what):
     loss, lse, grad = B.distill_loss(x, ids, y, grad_loss=w, want_grad=True)
     alone = B.distill_grad(x, lse, ids, y, grad_loss=w)
     assert loss[1] == 0 and math.isnan(lse[1]) and not grad[1].any() and not alone[1].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", list(BITS))
+@pytest.mark.parametrize("where", WHERE)
+@pytest.mark.parametrize("k", [0, 20])
+@pytest.mark.parametrize("rows,V,dtype", [(3, 33, BF16), (5, 5003, BF16), (5, 5003, F32), (1025, 5003, BF16), (1025, 20011, BF16), (4, 100003, BF16)])
+def test_log_probabilities(rows, V, dtype, k, where, what):
+    x = _logits(rows, V, dtype, rows)
+    tok = (torch.arange(rows, dtype=torch.int32, device="cuda") * 7 + 1) % V
+    clean = B.token_logprobs(x, tok, top_k=k)
+    _spoil(x, 1, where, what)
+    stats, ids, logps = B.token_logprobs(x, tok, top_k=k)
+    assert torch.isnan(stats[1]).all(), stats[1]
+    there = ids[1] >= 0
+    assert torch.isnan(logps[1][there]).all() and (logps[1][~there] == -math.inf).all()
+    # the alternatives are still the numbers in their order
+    s = x[1].float()
+    order = torch.sort(s.masked_fill(torch.isnan(s), -math.inf), descending=True, stable=True)
+    want = torch.where(order.values > -math.inf, order.indices, -1)[:k]
+    assert torch.equal(ids[1, :len(want)], want.int()) and (ids[1, len(want):] == -1).all()
+    others = [r for r in (0, 2, 3, rows - 1) if r < rows and r != 1]
+    assert all(_same(a, b, others) for a, b in zip((stats, ids, logps), clean))

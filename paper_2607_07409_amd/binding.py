@@ -598,7 +598,7 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, 
     q = exp(values) with renormalise=False (log probabilities, as token_logprobs gives them).  Entries with an id
     outside [0, V) or the value -inf are absent.  Returns (loss [rows], lse [rows], grad): with want_grad the
     gradient [rows, V] by the logits, each row weighted by grad_loss [rows] (None: 1), else None.  out: (loss, lse,
-    grad) to be overwritten; grad may be `logits` itself."""
+    grad) to be overwritten; grad may be `logits` itself, and is computed where it is given."""
     dev, f32 = logits.device, torch.float32
     stride, dtype = _row_stride(logits, "logits"), _dtype_code(logits)
     (rows, V), L = logits.shape, lib()
@@ -609,6 +609,8 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, 
             places = loss.data_ptr(), lse.data_ptr(), _address(grad), V
         else:
             loss, lse, grad = out
+            if want_grad and grad is None:
+                raise ValueError("want_grad, but out has no place for the gradient")
             places = (_vector(loss, "loss", (rows,), f32, dev), _vector(lse, "lse", (rows,), f32, dev),
                       *_grad_rows(grad, logits))
         ws, size = _scratch(workspace, L.dls_distill_workspace_size(rows, V), dev)
@@ -656,7 +658,8 @@ def head_distill(rho: torch.Tensor, w_vocab: torch.Tensor, ids: torch.Tensor, va
                  want_grads: bool = False, out=None, workspace=None, stream=None):
     """distill_loss of the logits rho @ w_vocab.T (bf16 [rows, r] and [V, r]), which are never stored.  Returns
     (loss [rows], lse [rows], d_rho [rows, r], d_w [V, r]); the gradients, of the rows' losses weighted by grad_loss
-    (None: 1), only with want_grads, else None.  out: these four, to be overwritten."""
+    (None: 1), only with want_grads, else None.  out: these four, to be overwritten; the gradients are computed where
+    they are given."""
     dev = rho.device
     if rho.dim() != 2 or w_vocab.dim() != 2:
         raise ValueError("rho must be [rows, r] and w_vocab [V, r]")
@@ -668,6 +671,8 @@ def head_distill(rho: torch.Tensor, w_vocab: torch.Tensor, ids: torch.Tensor, va
                    torch.empty((rows, r), dtype=bf16, device=dev) if want_grads else None,
                    torch.empty((V, r), dtype=bf16, device=dev) if want_grads else None)
         loss, lse, d_rho, d_w = out
+        if want_grads and (d_rho is None or d_w is None):
+            raise ValueError("want_grads, but out has no place for both gradients")
         teacher = _teacher(ids, values, rows, temperature, renormalise, dev)
         grads = int(d_rho is not None or d_w is not None)
         ws, size = _scratch(workspace, L.dls_head_distill_workspace_size(rows, V, r, teacher.k, grads), dev)

@@ -463,7 +463,8 @@ dls_status dls_distill_grad(const void *logits, dls_dtype dtype, int64_t rows, i
  *                sum_rows g loss by rho and by W, or both NULL (the loss alone)
  *   workspace    at least dls_head_distill_workspace_size bytes, 256-byte aligned; its content does
  *                not matter (with gradients: rows r 4 bytes for each of up to 256 splits of the
- *                vocabulary, 8 bytes a teacher entry twice, and small)
+ *                vocabulary, 16 bytes a teacher entry, V / 16 bytes for each 512 entries or, from 2^19 on,
+ *                64 V bytes, and small)
  * Products are exact and summed in float32; within the gradients each g / T (M p_v - q_v), a difference of float32 numbers,
  * counts to 2^-8 of itself, as the results do.  Results do not depend on anything but the arguments (no atomic sums).
  * Limits: 0 <= rows <= 2^20, 1 <= V <= 2^20, r a multiple of 8 with 8 <= r <= 256; finite rho and W. */

@@ -12,7 +12,8 @@ PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 OBJ_DIR = os.path.join(ROOT, "_build", "dels")
 LIB = os.path.join(PKG, "libdels.so")
-SOURCES = ["api.cpp", "api_distill.cpp", "token_logprobs.hip", "distill.hip", "head_distill.hip", "combine.hip", "draft.hip", "draft_small.hip", "accept.hip", "prepare.hip", "draft_persistent.hip", "prior.hip",
+SOURCES = ["api.cpp", "api_distill.cpp", "token_logprobs.hip", "distill.hip", "head_distill.hip", "combine.hip",
+           "draft.hip", "draft_small.hip", "accept.hip", "prepare.hip", "draft_persistent.hip", "prior.hip",
            "noalloc.hip", "uncertainty.hip", "peaks.hip",
            # the persistent kernel's instantiations, one unit per rank size and decoding mode
            "persist_greedy_r128.hip", "persist_greedy_r256.hip", "persist_sampled_r128.hip",

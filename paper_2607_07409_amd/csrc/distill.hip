@@ -2,13 +2,17 @@
 //   loss   = sum_k q_k (log q_k - log softmax(s / T)[id_k])
 //   d s_v  = g / T (M softmax(s / T)_v - sum_{k: id_k = v} q_k),   M = sum_k q_k, g the row's weight in the total.
 //
-// The loss needs the row's log-sum-exp, one pass over the logits (row_stream.hpp), and K entries.  The gradient is a
-// second pass that reads an entry and writes one; the teacher's entries of a workgroup's range are written after it,
-// each from its own logit in float32 and rounded once (several entries of one id by the first of them).
+// The loss needs the row's log-sum-exp, one pass over the logits (row_stream.hpp), and K entries.  Loss and gradient
+// together: a row that fits a workgroup's registers is read once and its gradient written from there (k_distill_row);
+// others take a second pass that reads an entry and writes one (k_distill_grad, which is also the gradient alone).  The
+// teacher's entries of a workgroup's range are written after it, each from its own logit in float32 and rounded once
+// (several entries of one id by the first of them).
 //
-// What bounds it: reads and writes.  2,048 bf16 rows of V = 151,936, loss and gradient in 243 to 254 us: 4.9 to 5.1 TB/s
+// What bounds it: reads and writes.  2,048 bf16 rows of V = 151,936, loss and gradient in 243 to 257 us: 4.8 to 5.1 TB/s
 // of the 1.24 GB read and written, where a large copy reaches 4.93.  The gradient alone of 777 rows of V = 70,001 in
-// 55.7 us (3.9 TB/s).  Small calls are latency: 16 rows of V = 32,003, loss and gradient, 8.9 us of kernel.
+// 55 us (3.9 TB/s), of 900 float32 rows of V = 81,920 in 125 (4.7).  Rows beyond the registers are read twice: 300
+// float32 rows of V = 151,936 in 120 us, 3.0 TB/s of what is read once and written (4.5 of what moves).  Small calls are
+// latency: 16 rows of V = 32,003, loss and gradient, 9 us of kernel.
 #include "teacher.hpp"
 
 namespace dls {

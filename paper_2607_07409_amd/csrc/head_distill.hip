@@ -26,10 +26,11 @@
 // wave a SIMD, so nothing but the wave itself hides its latencies: the streams run three tiles ahead, and the
 // exponentials of a tile stand between the matrix instructions of the tile before.
 //
-// Measured at 6,001 rows, V = 151,936, r = 256, K = 50: 1,644 to 1,706 us a call; in a profile k_head_rho 746 and k_head_w
-// 859 (two products of 467 GFLOP each: 1.25 and 1.09 PFLOP/s; a library product of 8192^3 reaches 1.20 to 1.52),
-// k_head_finish 36, the sort 54.  At 1,024 rows 416 us; 96 rows of V = 32,003, r = 128: 68 us, of which seven
-// launches and their ramps are most.  The loss alone of 256 rows: 37 to 39 us, W read once in 12.
+// Measured at 6,001 rows, V = 151,936, r = 256, K = 50: 1,641 to 1,777 us a call; in a profile k_head_rho 761 and k_head_w
+// 900 (two products of 467 GFLOP each: 1.23 and 1.04 PFLOP/s; a library product of 8192^3 reaches 1.20 to 1.52),
+// k_head_finish 49, the sort 51.  At 1,024 rows (K = 64) 411 to 432 us, k_head_rho 149 and k_head_w 224 of them (1.07 and
+// 0.71 PFLOP/s), k_head_finish 25; 96 rows of V = 32,003, r = 128: 68 us, of which seven launches and their ramps are
+// most.  The loss alone of 256 rows: 34 to 35 us, W read once in 12.
 #include "teacher.hpp"
 
 namespace dls {
@@ -301,7 +302,8 @@ __device__ __forceinline__ void acc_settle() { asm volatile("s_nop 15\n\ts_nop 1
 // sum_v bf16(2^(y_v - R)) W_v.  R is the largest of the first tile's y_v, and with GRAD all of the split's terms are
 // rounded as they stand above the R that is written: k_head_finish takes the roundings of the teacher's entries back.
 // Sums of up to 2^80 of what R stands for are as good as others; where one would pass that (55 nats above the first tile's
-// largest logit at T = 1), R moves, and the split is done over from the R that it ends with, at most once.
+// largest logit at T = 1), R moves, and the split is done over from the R that it ends with, at most once.  (Logits of
+// spread 3, 6,001 rows: 1,777 us at T = 1 and at 0.3, 2,715 at T = 0.1.)
 template <int D, bool GRAD>
 __global__ __launch_bounds__(kThreads, 1) void k_head_rho(const bf16_t* __restrict__ rho, const bf16_t* __restrict__ W,
                                                           int64_t rows, int V, int r, float c, int splits,
@@ -1012,8 +1014,8 @@ __global__ __launch_bounds__(kThreads) void k_zero(uint4* __restrict__ p, int64_
 // Workgroups at a time: one per CU, a wave of rank 256 or 128 with gradients holding its SIMD's registers, else two
 constexpr int kSlots = 256;
 int head_splits(int64_t rows, int V, bool grads) {
-  // of the vocabulary, where rho is held: a slot each; every split at least 4 tiles (46 rows at V = 9,176: 73 us a call,
-  // with at least 8 tiles 76)
+  // of the vocabulary, where rho is held: a slot each; every split at least 4 tiles (46 rows at V = 9,176: 77 us a call,
+  // with at least 8 tiles 79)
   const int64_t blocks = (rows + kHold - 1) / kHold;
   const int64_t cap = std::max<int64_t>(1, V / (4 * kTile)), slots = grads ? kSlots : 2 * kSlots;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / std::max<int64_t>(1, blocks), cap), kHeadMostSplits));
@@ -1076,7 +1078,7 @@ HeadLayout head_layout(int64_t rows, int32_t V, int32_t r, int32_t k, bool grads
   l.tiles = (V + kHold - 1) / kHold;
   l.keys = l.tiles * (kHold / kHeadGroup);   // every wave's, also past V
   // the tiles that the last round of workgroups has too few of share a slot's rows: parts of at least 4 tiles of rows
-  // (483 rows at V = 10,911: 110 us a call, with at least 8 tiles 138; 1,500 rows at V = 32,003: 228 either way)
+  // (483 rows at V = 10,911: 113 us a call, with at least 8 tiles 139; 1,500 rows at V = 32,003: 230 either way)
   const int left = l.tiles % kSlots;
   l.row_splits = left ? (int)std::max<int64_t>(1, std::min<int64_t>(kSlots / left, rows / (4 * kTile))) : 1;
   l.whole = l.row_splits > 1 ? l.tiles - left : l.tiles;

@@ -1,9 +1,9 @@
 // One pass over rows of logits: what the log-probability and distillation kernels share.
 //
-// A row of V entries is split into `parts` contiguous ranges, one workgroup of 256 threads each.  A thread reads
-// 16-byte chunks (coalesced over the workgroup; the next two are in flight while two are folded) and keeps, for
-// y = x c with c = log2(e) / T,
-//   R   the reference, the largest y so far (rounded as the entries' own products see it),
+// A row of V entries is split into `parts` contiguous ranges, one workgroup each (of 256 threads here; distillation with
+// its gradient also takes whole rows by 1,024).  A thread reads 16-byte chunks (coalesced over the workgroup; in row_chunks
+// the next U are in flight while U are folded) and keeps, for y = x c with c = log2(e) / T,
+//   R   the reference: a y that was the largest when it was taken, and is within kLazy of the largest so far,
 //   s   sum 2^(y - R),   and where the entropy is wanted   t = sum 2^(y - R) (y - R),
 // all in float32, so that log-sum-exp = ln2 (R + log2 s), log p = ln2 (y - R - log2 s) and H = ln2 (log2 s - t / s).
 // One fused multiply-add forms y - R with a single rounding, whatever the size of R.

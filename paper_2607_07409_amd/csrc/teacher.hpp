@@ -1,5 +1,5 @@
 // A teacher's top entries of a row, as the distillation kernels use them: K <= 256 (id, value) pairs, one per thread of
-// a workgroup of 256.  An entry whose id lies outside [0, V) or whose value is -inf (or NaN) is absent.
+// a workgroup of 256 threads or more.  An entry whose id lies outside [0, V) or whose value is -inf (or NaN) is absent.
 #pragma once
 #include "row_stream.hpp"
 

@@ -5,7 +5,7 @@
 // that there are many more blocks than k), and of each block the pass keeps the largest entry.
 // Ordered by (value, lower block first), the k-th of these block maxima bounds the row's k best entries from below: k
 // blocks hold an entry at least as good, so an entry of a block that ranks behind them is behind k others.  Only the k
-// best blocks are read again (512 bytes each, from the caches), their entries at or above the bound are collected in
+// best blocks are read again (512 bytes each, 128 in short parts, from the caches), their entries at or above the bound are collected in
 // LDS, and the k best of those are put in order.  Nothing in the pass depends on the data, so a row of equal entries
 // costs what any other does.  The first selections need not be exact: a few blocks more than k come along where that
 // saves a look at their keys.
@@ -14,9 +14,9 @@
 // the lower, so that the larger key is the better entry, ties going to the lower index, and no two are equal.  0 is
 // no key.  Masked entries (-inf) and NaN have none.
 //
-// What bounds it: many rows, the read (1,024 bf16 rows of V = 151,936 with their 20 best: 64 us a call; only reading
-// them takes 55, and 46 at the 6.75 TB/s that one large array is read with).  Few rows, the chain of launch, a part's
-// pass, its selection and the merge (16 such rows: 10.4 us the parts, 4.7 the merge; a row with its 5 best: 6.7 and 3.4).
+// What bounds it: many rows, the read (1,024 bf16 rows of V = 151,936 with their 20 best: 63 to 64 us a call; only
+// reading them takes 55, and 46 at the 6.75 TB/s that one large array is read with).  Few rows, the chain of launch, a part's
+// pass, its selection and the merge (16 such rows: 9.1 us the parts, 5.0 the merge; a row with its 5 best: 6.9 and 3.4).
 #include "row_stream.hpp"
 
 namespace dls {
@@ -372,8 +372,8 @@ hipError_t launch_t(const LogprobsArgs& a, hipStream_t st) {
   u64* keys = (u64*)(a.ws + l.off_keys);
   const T* L = (const T*)a.logits;
   // Long parts: four loads a thread in flight and, with alternatives, blocks of all four, so that they fit LDS.  Short
-  // ones: two (300 rows of V = 32,003: 17.5 us, with four 18.3).  Fine blocks where they fit (1,024 rows of V = 32,003:
-  // 24.2 us, else 25.0; 300 float32 rows with the 64 best: 21.9, else 24.2).
+  // ones: two (300 rows of V = 32,003: 17.1 us, with four 17.9).  Fine blocks where they fit (1,024 rows of V = 32,003:
+  // 24.0 us, else 24.6; 300 float32 rows with the 64 best: 22.0, else 22.6).
   const int64_t chunks = (a.V / Chunk<T>::N + parts - 1) / parts;
   const bool four = a.V / parts > 16384;
   const bool fine = (chunks + 1023) / 1024 * 1024 <= kBlocks * kBlockLanes;

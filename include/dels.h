@@ -419,7 +419,7 @@ dls_status dls_token_logprobs(const void *logits, dls_dtype dtype, int64_t rows,
  * loss 0 and gradient 0 (a position left out).  Entries of a row may repeat an id.  A masked student
  * entry (-inf) has p = 0; a teacher entry of positive weight there makes the loss +inf.  A student row with a NaN
  * or +inf has NaN for its loss, its log-sum-exp and its whole gradient (0 for loss and gradient where the row has
- * no teacher entries).  A teacher value of NaN counts as absent. */
+ * no teacher entries); one with NaN among its entries' values has NaN for its loss and its whole gradient. */
 #define DLS_TEACHER_LOGPROBS 0x1u
 typedef struct dls_teacher {
   const int32_t *ids;    /* [rows, k] device */

@@ -1,5 +1,5 @@
 // A teacher's top entries of a row, as the distillation kernels use them: K <= 256 (id, value) pairs, one per thread of
-// a workgroup of 256 threads or more.  An entry whose id lies outside [0, V) or whose value is -inf (or NaN) is absent.
+// a workgroup of 256 threads or more.  An entry whose id lies outside [0, V) or whose value is -inf is absent.
 #pragma once
 #include "row_stream.hpp"
 
@@ -44,11 +44,11 @@ __device__ __forceinline__ TeacherRaw teacher_raw(const TeacherArgs& te, int64_t
     const size_t at = (size_t)r * te.k + threadIdx.x;
     e.id = te.ids[at];
     e.y = te.values[at];
-    if (e.id < 0 || e.id >= V || !(e.y > -INFINITY)) e = TeacherRaw{-1, -INFINITY};
+    if (e.id < 0 || e.id >= V || e.y == -INFINITY) e = TeacherRaw{-1, -INFINITY};
   }
   return e;
 }
-// This thread's entry, and the row's mass sum_k q_k (1 or 0 where normalised).
+// This thread's entry, and the row's mass sum_k q_k (where normalised 1, 0 without entries, or NaN as the values are).
 template <int NT>
 __device__ __forceinline__ TeacherEntry teacher_entry(const TeacherArgs& te, TeacherRaw raw, TeacherShared<NT>& sh,
                                                       float* mass) {
@@ -62,16 +62,16 @@ __device__ __forceinline__ TeacherEntry teacher_entry(const TeacherArgs& te, Tea
     const float d = e.id < 0 ? -INFINITY : (raw.y - top) * te.c;   // (the largest finite values differ by a finite amount)
     const float w = fast_exp2(d);
     const float sum = block_sum<NT>(w, sh.red);
-    e.q = sum > 0.f ? w / sum : 0.f;
+    e.q = sum == 0.f ? 0.f : w / sum;
     e.log_q = e.id < 0 ? -INFINITY : (d - fast_log2(sum)) * kLn2;
-    *mass = sum > 0.f ? 1.f : 0.f;
+    *mass = sum == 0.f ? 0.f : sum / sum;
   }
   return e;
 }
 
 // q (log q - log p) of an entry; log2 of its probability is y - R - l2.  0 for an entry of weight 0.
 __device__ __forceinline__ float teacher_term(const TeacherEntry& e, float log2_p) {
-  return e.q > 0.f ? e.q * (e.log_q - log2_p * kLn2) : 0.f;
+  return e.q == 0.f ? 0.f : e.q * (e.log_q - log2_p * kLn2);
 }
 
 }  // namespace dls

@@ -81,3 +81,30 @@ def test_log_probabilities(rows, V, dtype, k, where, what):
     assert torch.equal(ids[1, :len(want)], want.int()) and (ids[1, len(want):] == -1).all()
     others = [r for r in (0, 2, 3, rows - 1) if r < rows and r != 1]
     assert all(_same(a, b, others) for a, b in zip((stats, ids, logps), clean))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("renorm,value", [(True, math.nan), (True, math.inf), (False, math.nan)])
+@pytest.mark.parametrize("rows,V,dtype", [(5, 5003, BF16), (600, 5003, F32), (4, 100003, BF16)])
+def test_a_teacher_that_is_not_a_number(rows, V, dtype, renorm, value):
+    """One value of a row's entries (its id inside the vocabulary): loss and gradient of that row are NaN, the others' as they are."""
+    K, g = 9, torch.Generator().manual_seed(V)
+    x = _logits(rows, V, dtype, rows)
+    ids = torch.randint(0, V, (rows, K), generator=g, dtype=torch.int32).cuda()
+    y = torch.log_softmax(torch.randn((rows, K), generator=g), 1).cuda()
+    clean = B.distill_loss(x, ids, y, renormalise=renorm, want_grad=True)
+    y[1, 4] = value
+    loss, lse, grad = B.distill_loss(x, ids, y, renormalise=renorm, want_grad=True)
+    alone = B.distill_grad(x, lse, ids, y, renormalise=renorm)
+    assert math.isnan(loss[1]) and torch.isnan(grad[1]).all() and torch.isnan(alone[1]).all()
+    others = [0, 2, 3, rows - 1]
+    assert torch.equal(lse, clean[1]) and _same(loss, clean[0], others) and _same(grad, clean[2], others)
+    rho, w = _logits(rows, 64, BF16, 1), _logits(997, 64, BF16, 2) / 8
+    ids %= 997
+    clean = B.head_distill(rho, w, ids, torch.where(torch.isfinite(y), y, 0.0), renormalise=renorm, want_grads=True)
+    loss, lse, d_rho, d_w = B.head_distill(rho, w, ids, y, renormalise=renorm, want_grads=True)
+    assert math.isnan(loss[1]) and torch.isnan(d_rho[1]).all() and torch.isnan(d_w).all()
+    assert torch.equal(lse, clean[1]) and _same(loss, clean[0], others) and _same(d_rho, clean[2], others)
+    # outside the vocabulary it is absent
+    ids[1, 4] = 997
+    assert torch.isfinite(B.head_distill(rho, w, ids, y, renormalise=renorm)[0]).all()
